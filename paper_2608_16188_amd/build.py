@@ -3,9 +3,9 @@
     python -m paper_2608_16188_amd.build
 
 Each source compiles on its own (in parallel) into _build/, then links into
-paper_2608_16188_amd/libvmoe.so. route.hip and grouping.cpp (host code) are
-compiled without floating-point contraction: their arithmetic is specified
-operation by operation.
+paper_2608_16188_amd/libvmoe.so. route.hip, adamw.hip and grouping.cpp (host
+code) are compiled without floating-point contraction: their arithmetic is
+specified operation by operation.
 """
 from __future__ import annotations
 
@@ -21,10 +21,11 @@ LIB = os.path.join(PKG, "libvmoe.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["abi.hip", "route.hip", "moves.hip", "ffn.hip", "route_bwd.hip", "balance.hip",
-           "grouping.cpp"]
+           "abi_train.hip", "block_norm.hip", "gate_loss.hip", "adamw.hip", "grouping.cpp"]
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-PER_FILE = {"route.hip": ["-ffp-contract=off"], "grouping.cpp": ["-ffp-contract=off"]}
+PER_FILE = {"route.hip": ["-ffp-contract=off"], "grouping.cpp": ["-ffp-contract=off"],
+            "adamw.hip": ["-ffp-contract=off"]}
 
 
 def build(verbose: bool = False) -> str:
