@@ -140,13 +140,21 @@ vmoe_status vmoe_load_balance_loss(const vmoe_shape* shape, const float* logits,
  * 2^(s - 127) u, u from its byte with 3 mantissa bits M and an exponent X:
  *   m: sign bit, 4-bit X, M;  u = +-2^(X - 15) (1 + M/8), +-2^-14 M/8 for X = 0
  *   v:           5-bit X, M;  u =   2^(X - 31) (1 + M/8),   2^-30 M/8 for X = 0
- * s is the exponent of the block's largest magnitude after rounding up to 3
- * mantissa bits, 0 for a block of zeros (or of values below 2^-126) and 255 for
- * one that holds an infinity or NaN: that block reads as NaN from then on.
+ * s is the f32 exponent field of the block's largest magnitude after rounding it
+ * up to 3 mantissa bits (0 for a block of zeros or of values below 2^-126).
+ * Where that overflows, or the block holds an infinity or NaN, s is 255 and the
+ * whole block reads as infinite from then on.
  * Elements are rounded at random, up with the probability of what is cut off,
  * so a moment's expected value is its exact one however small a step's change
  * is (rounding to nearest would freeze v, which changes by a thousandth a step);
- * a positive v never becomes 0, so that no m is divided by an emptied v. */
+ * a positive v never becomes 0, so that no m is divided by an emptied v.
+ * The random numbers are a function of seed, step and the element's number i
+ * (index0 + its place) alone, in 32-bit arithmetic:
+ *   mix(x): x ^= x >> 16; x *= 0x6A09E667; x ^= x >> 15; x *= 0xBB67AE85; x ^= x >> 16
+ *   key = mix(seed ^ mix(step 0x9E3779B1)), and mix(key ^ (i >> 32)) where i >= 2^32
+ *   bits = mix((i 0x9E3779B1) ^ key); its low 16 bits are m's, the high ones v's
+ * and an element whose cut-off fraction is q of a step goes up where
+ * q + (16 bits + 1/2) / 2^16 >= 1. */
 typedef enum { VMOE_STATE_F32 = 0, VMOE_STATE_8BIT = 1 } vmoe_adamw_state;
 
 typedef struct vmoe_adamw_tensor {
@@ -208,8 +216,8 @@ size_t vmoe_grad_norm_workspace_bytes(int64_t n_chunks);
  * finite (a gradient is not, or its square leaves the range of f32): vmoe_adamw
  * given that clip changes nothing. max_norm > 0 (infinity: the norm alone).
  * plan: device copy of the plan, n_chunks as from vmoe_adamw_plan_chunks;
- * clip [2] f32, device, out. Squares are summed in f32 by a thread (at most
- * a few hundred) and by a block, in double across blocks. */
+ * clip [2] f32, device, out. Squares are summed in f32 over a
+ * thread's 32 elements of a chunk, in double beyond. */
 vmoe_status vmoe_grad_norm(const void* plan, int64_t n_chunks, double grad_scale, double max_norm,
                            float* clip, void* workspace, size_t workspace_bytes, void* stream);
 

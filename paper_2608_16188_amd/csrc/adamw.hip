@@ -308,8 +308,9 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
 }
 
 template <bool BF16>
-__device__ __forceinline__ float chunk_squares(const Entry& e, float s) {
+__device__ __forceinline__ float chunk_squares(const Entry& e) {
     const int n = e.count, tid = threadIdx.x;
+    float s = 0.0f;
     constexpr int U = 4;
     int base = 0;
     for (; base + U * kSpan <= n; base += U * kSpan) {
@@ -334,10 +335,10 @@ __global__ __launch_bounds__(kThreads) void norm_partial_kernel(const Entry* __r
                                                                 long long n_chunks,
                                                                 double* __restrict__ partial) {
     __shared__ double lds[kThreads / 64];
-    float s = 0.0f;
+    double s = 0.0;
     for (long long c = blockIdx.x; c < n_chunks; c += gridDim.x) {
         const Entry& e = plan[c];
-        s = (e.flags & kGradBf16) ? chunk_squares<true>(e, s) : chunk_squares<false>(e, s);
+        s += (e.flags & kGradBf16) ? chunk_squares<true>(e) : chunk_squares<false>(e);
     }
     const double t = block_sum(s, lds);
     if (threadIdx.x == 0) partial[blockIdx.x] = t;

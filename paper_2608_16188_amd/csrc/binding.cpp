@@ -11,6 +11,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstring>
 #include <exception>
 #include <vector>
 
@@ -82,11 +83,17 @@ void* stream_of(PyObject* o) {
     return s;
 }
 
-// A ctypes structure's memory.
+// Memory of a ctypes structure, told from others (of the same size) by its
+// class's name.
 template <typename T>
 struct Shape {
     Py_buffer view;
-    explicit Shape(PyObject* o) {
+    Shape(PyObject* o, const char* name) {
+        if (strcmp(Py_TYPE(o)->tp_name, name) != 0) {
+            PyErr_Format(PyExc_TypeError, "shape: a %s is wanted, got %s", name,
+                         Py_TYPE(o)->tp_name);
+            throw Refused();
+        }
         if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Refused();
         if (view.len != static_cast<Py_ssize_t>(sizeof(T))) {
             PyBuffer_Release(&view);
@@ -135,7 +142,7 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t wanted, F f) {
 
 PyObject* block_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 14, [&] {
-        const Shape<vmoe_norm_shape> s(a[0]);
+        const Shape<vmoe_norm_shape> s(a[0], "NormShape");
         const at::ScalarType act = scalar(s->dtype), res = scalar(s->stream_dtype);
         const int64_t d = s->d_model, rows = s->n_tokens, all = rows * d;
         void* const p[] = {
@@ -153,7 +160,7 @@ PyObject* block_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 21, [&] {
-        const Shape<vmoe_norm_shape> s(a[0]);
+        const Shape<vmoe_norm_shape> s(a[0], "NormShape");
         const at::ScalarType act = scalar(s->dtype), res = scalar(s->stream_dtype);
         const int64_t d = s->d_model, rows = s->n_tokens, all = rows * d;
         void* const p[] = {
@@ -176,7 +183,7 @@ PyObject* block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* load_balance_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 15, [&] {
-        const Shape<vmoe_shape> s(a[0]);
+        const Shape<vmoe_shape> s(a[0], "Shape");
         const int64_t rows = s->n_tokens, E = s->n_experts, G = s->n_groups;
         void* const p[] = {
             pointer(a[1], "logits", kF32, rows * E), pointer(a[2], "logit_bias", kF32, E),
