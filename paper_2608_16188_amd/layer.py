@@ -125,11 +125,12 @@ class LayerBuffers:
                            self.y, stream)
 
     def backward(self, stream=None, fused: bool = True, quota: bool = False,
-                 gather: bool = False):
+                 gather: bool = False, dlogits=None):
         """fused: dispatch and router backward in one call (bit-identical to
         vmoe_dispatch_bwd followed by vmoe_route_bwd, which fused=False runs);
         quota: the expert MLP backward through the fill-clamp-refill tile
-        scheduler."""
+        scheduler; dlogits: an auxiliary loss's gradient at the router logits,
+        added to the gate's (fused only)."""
         s = self.shape
         V.vmoe_combine_bwd(s, self.dy, self.ye, self.expert_idx, self.slot, self.row_base,
                            self.gate, self.dye, self.dgate, stream)
@@ -141,6 +142,14 @@ class LayerBuffers:
             ffn = V.vmoe_expert_ffn_bwd_quota if quota else V.vmoe_expert_ffn_bwd
             ffn(s, self.xe, self.counts, self.w1, self.w2, self.a, self.a_grad, self.dye,
                 self.dh, self.dxe, self.dw1, self.db1, self.dw2, self.db2, stream)
+        if dlogits is not None:
+            if not fused:
+                raise ValueError("dlogits needs the fused backward")
+            V.vmoe_dispatch_route_bwd_dlogits(s, self.dxe, self.row_base, self.x, self.w_router,
+                                              self.probs, self.expert_idx, self.slot, self.dgate,
+                                              dlogits, self.dx, self.dw_router, self.route_bwd_ws,
+                                              stream)
+            return
         if fused:
             V.vmoe_dispatch_route_bwd(s, self.dxe, self.row_base, self.x, self.w_router,
                                       self.probs, self.expert_idx, self.slot, self.dgate, self.dx,
