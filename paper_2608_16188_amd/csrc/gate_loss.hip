@@ -3,18 +3,24 @@
 //   L_balance = E sum_e f_e P_e, f_e = demand_e / (k n), P_e = mean of probs;
 //   L_z       = mean of lse^2, lse = log sum_e exp z;
 //   dlogits   = p (w_balance E (f - <f, p>) + 2 w_z lse) / n.
-// The gradient needs f of the whole group, so there are two passes. The first
-// reads logits, noise, probs and choices once: a chunk's counts, sums of probs
-// and of lse^2, and each token's lse, for which the softmax's largest term is
-// enough (lse = max z - log max p: no second exponential). The second adds the
-// group's counts (integers, a few hundred short rows from L2) in every block
-// and forms the rows of dlogits from probs and lse; one more block a group adds
-// the other sums, in double and in chunk order, and writes the losses. A group
-// of few tokens runs both passes in one block of one launch.
-// A lane holds four consecutive experts of a token (one 16-byte access where E
-// is a multiple of 4), so a token takes at most 16 lanes and its maxima and sums
-// are moves within a row of lanes, without LDS. Both passes are bound by latency
-// up to some ten thousand tokens, by HBM beyond.
+// The gradient needs f of the whole group, and f needs the choices alone. Three
+// ways, by size:
+// - a group of few tokens: one block does everything, in one launch;
+// - rows of up to 16 MB: a first launch takes a chunk's counts, sums of probs and
+//   of lse^2 and each token's lse, a second adds the group's counts in every
+//   block and writes dlogits from probs (read again) and lse, with one more
+//   block a group for the losses beside them;
+// - more: a first launch counts the choices (a small part of the bytes), a second
+//   reads logits, noise and probs once, writes dlogits and leaves sums, and a
+//   third writes the losses. Reading probs again would cost more than a launch
+//   (61 x 4093 tokens of 64 experts: 51 us, 62 in two launches; 36928 of 32: 17
+//   against 12).
+// Sums over chunks are in double and in a fixed order. The softmax's largest term
+// is enough for lse = max z - log max p: no second exponential. A lane holds four
+// consecutive experts of a token (one 16-byte access where E is a multiple of 4),
+// so a token takes at most 16 lanes and its maxima and sums are moves within a
+// row of lanes, without LDS. Bound by latency up to some ten thousand tokens, by
+// HBM beyond.
 #include <type_traits>
 
 #include "common_train.h"
@@ -22,11 +28,13 @@
 namespace vmoe {
 namespace {
 
-constexpr int kSteps = 4;        // token steps whose loads are in flight together
-constexpr int kChunkWaves = 8;   // waves of a block that takes a chunk
-constexpr int kGroupWaves = 16;  // of a block that takes a whole group
-constexpr int kBlocks = 1024;    // most chunks over all groups (but one a group)
-constexpr int kGroupChunks = 256;  // and of one group
+constexpr int kSteps = 4;          // token steps whose loads are in flight together
+constexpr int kChunkWaves = 8;     // waves of a block that takes a chunk
+constexpr int kGroupWaves = 16;    // of a block that takes a whole group
+constexpr int kBlocks = 512;      // most chunks over all groups (but one a group)
+constexpr int kGroupChunks = 256;  // most of one group whose counts other blocks add
+constexpr int kCountTokens = 512;  // fewest tokens of a part that is only counted
+constexpr long long kRereadBytes = 16LL << 20;  // most bytes of probs that are read twice
 
 // EMAX (a power of two >= E) / 4 lanes hold a token's row.
 template <int EMAX, int WAVES>
@@ -43,11 +51,12 @@ struct LossArgs {
     const float *logits, *bias, *noise, *probs;
     const int32_t* idx;
     const uint8_t* mask;
-    float *lse, *sum_p, *sum_z;      // workspace: [N], [G, chunks, EMAX], [G, chunks]
-    int32_t *counts, *live;          // workspace: [G, chunks, EMAX], [G, chunks]
+    float *sum_p, *sum_z;      // workspace: [G, chunks, EMAX], [G, chunks]
+    float* lse;                // workspace: [N] where probs are read twice
+    int32_t *counts, *live;    // workspace: [G, parts, EMAX], [G, parts]
     float *losses, *mean_probs, *dlogits;
     int32_t* demand;
-    int Ng, E, k, chunks, chunk_tokens;
+    int Ng, E, k, chunks, chunk_tokens, parts, part_tokens;
     float w_balance, w_z;
 };
 
@@ -90,146 +99,116 @@ __device__ __forceinline__ bool kept(const LossArgs& a, size_t t) {
     return a.mask == nullptr || a.mask[t] != 0;
 }
 
-// A block's sums over tokens [t0, t1) of its group.
+// Choices and tokens of [t0, t1) of a group that starts at token `first`, by a
+// block: choices in rows of consecutive words, counted by integer LDS atomics
+// on counts of the wave's own.
 template <int EMAX, int WAVES>
-struct BlockSums {
+struct Counts {
     int hist[WAVES][EMAX];
-    float p[WAVES][EMAX];
-    float z[WAVES];
     int n[WAVES];
-    __device__ __forceinline__ int count(int e) const {
+    __device__ __forceinline__ int choices(int e) const {
         int t = 0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) t += hist[w][e];
         return t;
     }
+    __device__ __forceinline__ int tokens() const {
+        int t = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) t += n[w];
+        return t;
+    }
+};
+
+template <int EMAX, int WAVES>
+__device__ __forceinline__ void count(const LossArgs& a, size_t first, int t0, int t1,
+                                      Counts<EMAX, WAVES>& c) {
+    constexpr int kThreads = 64 * WAVES;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int i = lane; i < EMAX; i += 64) c.hist[wave][i] = 0;
+    const int words = (t1 - t0) * a.k;
+    const int32_t* idx = a.idx + (first + t0) * a.k;
+    for (int b = tid; b < words; b += kSteps * kThreads) {
+        int x[kSteps];
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            const int w = b + u * kThreads;
+            x[u] = w < words && kept(a, first + t0 + w / a.k) ? idx[w] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u)
+            if (x[u] >= 0 && x[u] < a.E) atomicAdd(&c.hist[wave][x[u]], 1);
+    }
+    int n = t1 - t0;
+    if (a.mask != nullptr) {
+        n = 0;
+        for (int t = t0 + tid; t < t1; t += kThreads) n += kept(a, first + t) ? 1 : 0;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+    } else if (wave != 0) {
+        n = 0;
+    }
+    if (lane == 0) c.n[wave] = n;
+    __syncthreads();
+}
+
+// A block's sums of probs and lse^2.
+template <int EMAX, int WAVES>
+struct Sums {
+    float p[WAVES][EMAX];
+    float z[WAVES];
     __device__ __forceinline__ float prob(int e) const {
         float t = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) t += p[w][e];
         return t;
     }
-    __device__ __forceinline__ float square(float s = 0.0f) const {
+    __device__ __forceinline__ float square() const {
+        float t = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) s += z[w];
-        return s;
-    }
-    __device__ __forceinline__ int tokens(int s = 0) const {
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) s += n[w];
-        return s;
+        for (int w = 0; w < WAVES; ++w) t += z[w];
+        return t;
     }
 };
 
-// lse of token t to lse[t - t0]. Ends with a barrier.
-template <int EMAX, int WAVES>
-__device__ __forceinline__ void sum_tokens(const LossArgs& a, size_t first, int t0, int t1,
-                                           BlockSums<EMAX, WAVES>& sums, float* lse) {
+// What a pass over rows does: the block's sums and lse, dlogits from lse, or both
+// at once (lse is not stored).
+enum Pass { kSums, kGradient, kBoth };
+
+// Rows [t0, t1). `ready` runs between the first rows' loads and their use and
+// sets 1 / n and the lane's four f (not for kSums). Ends with a barrier, unless
+// kGradient.
+template <int EMAX, int WAVES, Pass PASS, typename F>
+__device__ __forceinline__ void do_rows(const LossArgs& a, size_t first, int t0, int t1,
+                                        Sums<EMAX, WAVES>* sums, F ready) {
     using R = Rows<EMAX, WAVES>;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int e0 = (lane % R::kLanes) * 4, sub = lane / R::kLanes;
-    // the first choices are requested before the rows
-    const int words = (t1 - t0) * a.k;
-    const int32_t* idx = a.idx + (first + t0) * a.k;
-    int x[kSteps];
-    const auto choices = [&](int b) {
-#pragma unroll
-        for (int u = 0; u < kSteps; ++u) {
-            const int w = b + u * R::kThreads;
-            x[u] = w < words && kept(a, first + t0 + w / a.k) ? idx[w] : -1;
-        }
-    };
-    choices(tid);
-    for (int i = lane; i < EMAX; i += 64) sums.hist[wave][i] = 0;
     const float4 be = a.bias ? load_row(a.bias, e0, a.E, true) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float bv[4] = {be.x, be.y, be.z, be.w};
+    float f4[4] = {0.0f, 0.0f, 0.0f, 0.0f}, cb = 0.0f, cz = 0.0f;
     float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, acc_z = 0.0f;
-    int acc_n = 0;
     for (int b = t0; b < t1; b += kSteps * R::kBlockTokens) {
         float4 l[kSteps], nz[kSteps], p[kSteps];
+        float ls[kSteps];
         bool on[kSteps];
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
             const int t = b + (u * WAVES + wave) * R::kTokens + sub;
             on[u] = t < t1 && kept(a, first + t);
             const size_t q = (first + t) * a.E;
-            l[u] = load_row(a.logits + q, e0, a.E, on[u]);
             p[u] = load_row(a.probs + q, e0, a.E, on[u]);
-            nz[u] = load_row(a.noise + q, e0, a.E, on[u] && a.noise != nullptr);
-        }
-#pragma unroll
-        for (int u = 0; u < kSteps; ++u) {
-            const int t = b + (u * WAVES + wave) * R::kTokens + sub;
-            const float lv[4] = {l[u].x, l[u].y, l[u].z, l[u].w};
-            const float nv[4] = {nz[u].x, nz[u].y, nz[u].z, nz[u].w};
-            const float pv[4] = {p[u].x, p[u].y, p[u].z, p[u].w};
-            const float bv[4] = {be.x, be.y, be.z, be.w};
-            float top = -INFINITY, most = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float z = a.bias ? lv[j] + bv[j] : lv[j];
-                if (a.noise) z += nv[j];
-                if (e0 + j < a.E) top = fmaxf(top, z);
-                most = fmaxf(most, pv[j]);
-                acc[j] += pv[j];
-            }
-            top = over_token<R::kLanes>(top, Max{});
-            most = over_token<R::kLanes>(most, Max{});
-            if (on[u] && e0 == 0) {
-                const float v = top - logf(most);
-                acc_z = __builtin_fmaf(v, v, acc_z);
-                acc_n += 1;
-                lse[t - t0] = v;
+            if constexpr (PASS == kGradient) {
+                ls[u] = on[u] ? a.lse[first + t] : 0.0f;
+            } else {
+                l[u] = load_row(a.logits + q, e0, a.E, on[u]);
+                nz[u] = a.noise ? load_row(a.noise + q, e0, a.E, on[u])
+                                : make_float4(0.f, 0.f, 0.f, 0.f);
             }
         }
-    }
-#pragma unroll
-    for (int o = 32; o >= R::kLanes; o >>= 1)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], o);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        acc_z += __shfl_xor(acc_z, o);
-        acc_n += __shfl_xor(acc_n, o);
-    }
-    if (sub == 0)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sums.p[wave][e0 + j] = acc[j];
-    if (lane == 0) {
-        sums.z[wave] = acc_z;
-        sums.n[wave] = acc_n;
-    }
-    // choices in rows of consecutive words; integer LDS atomics on the wave's
-    // own counts
-    for (int b = tid; b < words; b += kSteps * R::kThreads) {
-        if (b != tid) choices(b);
-#pragma unroll
-        for (int u = 0; u < kSteps; ++u)
-            if (x[u] >= 0 && x[u] < a.E) atomicAdd(&sums.hist[wave][x[u]], 1);
-    }
-    __syncthreads();
-}
-
-// Rows [t0, t1) of dlogits; f4: the lane's four f, per: 1 / n. `ready` runs
-// between the first rows' loads and their use, and sets f4 and per.
-template <int EMAX, int WAVES, typename F>
-__device__ __forceinline__ void write_rows(const LossArgs& a, size_t first, int t0, int t1,
-                                           const float* lse, F ready) {
-    using R = Rows<EMAX, WAVES>;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int e0 = (lane % R::kLanes) * 4, sub = lane / R::kLanes;
-    float f4[4], per = 0.0f, cb = 0.0f, cz = 0.0f;
-    for (int b = t0; b < t1; b += kSteps * R::kBlockTokens) {
-        float4 p[kSteps];
-        float ls[kSteps];
-#pragma unroll
-        for (int u = 0; u < kSteps; ++u) {
-            const int t = b + (u * WAVES + wave) * R::kTokens + sub;
-            const bool on = t < t1 && kept(a, first + t);
-            p[u] = load_row(a.probs + (first + t) * a.E, e0, a.E, on);
-            ls[u] = on ? lse[t - t0] : 0.0f;
-        }
-        if (b == t0) {
-            ready(f4, per);
+        if (PASS != kSums && b == t0) {
+            float per;
+            ready(e0, f4, per);
             cb = a.w_balance * static_cast<float>(a.E) * per;
             cz = 2.0f * a.w_z * per;
         }
@@ -237,6 +216,30 @@ __device__ __forceinline__ void write_rows(const LossArgs& a, size_t first, int 
         for (int u = 0; u < kSteps; ++u) {
             const int t = b + (u * WAVES + wave) * R::kTokens + sub;
             const float pv[4] = {p[u].x, p[u].y, p[u].z, p[u].w};
+            float lse = 0.0f;
+            if constexpr (PASS == kGradient) {
+                lse = ls[u];
+            } else {
+                const float lv[4] = {l[u].x, l[u].y, l[u].z, l[u].w};
+                const float nv[4] = {nz[u].x, nz[u].y, nz[u].z, nz[u].w};
+                float top = -INFINITY, most = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float z = a.bias ? lv[j] + bv[j] : lv[j];
+                    if (a.noise) z += nv[j];
+                    if (e0 + j < a.E) top = fmaxf(top, z);
+                    most = fmaxf(most, pv[j]);
+                    acc[j] += pv[j];
+                }
+                top = over_token<R::kLanes>(top, Max{});
+                most = over_token<R::kLanes>(most, Max{});
+                if (on[u]) lse = top - logf(most);
+                if (e0 == 0) {
+                    acc_z = __builtin_fmaf(lse, lse, acc_z);
+                    if (PASS == kSums && on[u]) a.lse[first + t] = lse;
+                }
+            }
+            if constexpr (PASS == kSums) continue;
             float inner = 0.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) inner = __builtin_fmaf(f4[j], pv[j], inner);
@@ -244,7 +247,7 @@ __device__ __forceinline__ void write_rows(const LossArgs& a, size_t first, int 
             float d[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                d[j] = pv[j] * __builtin_fmaf(cb, f4[j] - inner, cz * ls[u]);
+                d[j] = pv[j] * __builtin_fmaf(cb, f4[j] - inner, cz * lse);
             if (t < t1 && e0 < a.E) {
                 float* out = a.dlogits + (first + t) * a.E + e0;
                 if (a.E % 4 == 0) {
@@ -257,10 +260,30 @@ __device__ __forceinline__ void write_rows(const LossArgs& a, size_t first, int 
             }
         }
     }
+    if constexpr (PASS == kGradient) return;
+#pragma unroll
+    for (int o = 32; o >= R::kLanes; o >>= 1)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], o);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) acc_z += __shfl_xor(acc_z, o);
+    if (sub == 0)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums->p[wave][e0 + j] = acc[j];
+    if (lane == 0) sums->z[wave] = acc_z;
+    __syncthreads();
 }
 
-// Demand, mean probabilities and losses of a group from its totals in LDS, by a
-// whole block.
+// The lane's four f and 1 / n from a group's totals in LDS.
+__device__ __forceinline__ void shares(const LossArgs& a, const int* total, int n_live, int e0,
+                                       float (&f4)[4], float& per) {
+    per = n_live > 0 ? 1.0f / static_cast<float>(n_live) : 0.0f;
+    const float fk = per / static_cast<float>(a.k);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f4[j] = static_cast<float>(total[e0 + j]) * fk;
+}
+
+// Demand, mean probabilities and losses of a group, by a whole block.
 __device__ __forceinline__ void write_losses(const LossArgs& a, int g, const int* total,
                                              const double* sum_p, double sum_z, int n_live) {
     const int tid = threadIdx.x;
@@ -283,69 +306,70 @@ __device__ __forceinline__ void write_losses(const LossArgs& a, int g, const int
     }
 }
 
-__device__ __forceinline__ void shares(const LossArgs& a, const int* total, int n_live, int e0,
-                                       float (&f4)[4], float& per) {
-    per = n_live > 0 ? 1.0f / static_cast<float>(n_live) : 0.0f;
-    const float fk = per / static_cast<float>(a.k);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f4[j] = static_cast<float>(total[e0 + j]) * fk;
-}
-
 // A whole group in one block.
 template <int EMAX>
 __global__ __launch_bounds__(64 * kGroupWaves) void gate_group_kernel(LossArgs a) {
-    using R = Rows<EMAX, kGroupWaves>;
-    __shared__ BlockSums<EMAX, kGroupWaves> sums;
-    __shared__ float lse[R::kGroupTokens];
+    __shared__ Counts<EMAX, kGroupWaves> counts;
+    __shared__ Sums<EMAX, kGroupWaves> sums;
     __shared__ int total[EMAX];
     __shared__ double sum_p[EMAX];
     const int g = blockIdx.x, tid = threadIdx.x;
     const size_t first = static_cast<size_t>(g) * a.Ng;
-    sum_tokens<EMAX, kGroupWaves>(a, first, 0, a.Ng, sums, lse);
-    const int n_live = sums.tokens();
-    if (tid < EMAX) {
-        total[tid] = sums.count(tid);
-        sum_p[tid] = sums.prob(tid);
-    }
+    int n_live = 0;
+    const auto totals = [&] {
+        count<EMAX, kGroupWaves>(a, first, 0, a.Ng, counts);
+        n_live = counts.tokens();
+        if (tid < EMAX) total[tid] = counts.choices(tid);
+        __syncthreads();
+    };
+    if (a.Ng == 0) totals();  // no rows to call it
+    do_rows<EMAX, kGroupWaves, kBoth>(a, first, 0, a.Ng, &sums,
+                                      [&](int e0, float (&f4)[4], float& per) {
+                                          totals();
+                                          shares(a, total, n_live, e0, f4, per);
+                                      });
+    if (tid < EMAX) sum_p[tid] = sums.prob(tid);
     __syncthreads();
-    write_rows<EMAX, kGroupWaves>(a, first, 0, a.Ng, lse, [&](float (&f4)[4], float& per) {
-        shares(a, total, n_live, ((tid & 63) % R::kLanes) * 4, f4, per);
-    });
     write_losses(a, g, total, sum_p, sums.square(), n_live);
 }
 
-// First pass over a chunk.
-template <int EMAX>
-__global__ __launch_bounds__(64 * kChunkWaves) void gate_sums_kernel(LossArgs a) {
-    __shared__ BlockSums<EMAX, kChunkWaves> sums;
-    const int g = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, tid = threadIdx.x;
-    const int t0 = chunk * a.chunk_tokens, t1 = min(t0 + a.chunk_tokens, a.Ng);
-    const size_t first = static_cast<size_t>(g) * a.Ng;
-    sum_tokens<EMAX, kChunkWaves>(a, first, t0, t1, sums, a.lse + first + t0);
+// Counts of one part of a group's choices; with them, where probs are read twice,
+// the part's sums and lse.
+template <int EMAX, bool SUMS>
+__global__ __launch_bounds__(64 * kChunkWaves) void gate_count_kernel(LossArgs a) {
+    __shared__ Counts<EMAX, kChunkWaves> counts;
+    __shared__ Sums<EMAX, kChunkWaves> sums;
+    const int g = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
+    const int t0 = part * a.part_tokens, t1 = min(t0 + a.part_tokens, a.Ng);
+    const size_t first = static_cast<size_t>(g) * a.Ng, row = blockIdx.x;
+    if constexpr (SUMS)
+        do_rows<EMAX, kChunkWaves, kSums>(a, first, t0, t1, &sums,
+                                          [](int, float (&)[4], float&) {});
+    count<EMAX, kChunkWaves>(a, first, t0, t1, counts);
     if (tid < EMAX) {
-        a.sum_p[static_cast<size_t>(blockIdx.x) * EMAX + tid] = sums.prob(tid);
-        a.counts[static_cast<size_t>(blockIdx.x) * EMAX + tid] = sums.count(tid);
+        a.counts[row * EMAX + tid] = counts.choices(tid);
+        if constexpr (SUMS) a.sum_p[row * EMAX + tid] = sums.prob(tid);
     }
     if (tid == 64) {
-        a.sum_z[blockIdx.x] = sums.square();
-        a.live[blockIdx.x] = sums.tokens();
+        a.live[row] = counts.tokens();
+        if constexpr (SUMS) a.sum_z[row] = sums.square();
     }
 }
 
-// The group's counts and its number of tokens: rows of EMAX counts as a flat run
-// of 16-byte words, of which a thread always meets the same four experts (4
-// threads' worth of a block is a multiple of EMAX). Ends with a barrier.
+// A group's counts and its number of tokens: rows of EMAX counts as a flat run
+// of 16-byte words, of which a thread always meets the same four experts (four
+// times a block's threads is a multiple of EMAX). Ends with a barrier.
 template <int EMAX>
 __device__ __forceinline__ void group_counts(const LossArgs& a, int g, int* total, int& n_live) {
-    constexpr int kQuads = EMAX / 4, kThreads = 64 * kChunkWaves, kFlight = 16;
+    constexpr int kQuads = EMAX / 4, kThreads = 64 * kChunkWaves, kFlight = 4;
+    static_assert(kGroupChunks <= kThreads, "a thread takes one part's tokens");
     __shared__ int part[kChunkWaves][EMAX];
     __shared__ int part_n[kChunkWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int4* rows = reinterpret_cast<const int4*>(a.counts +
-                                                     static_cast<size_t>(g) * a.chunks * EMAX);
-    const int words = a.chunks * kQuads;
-    int n = 0;
-    for (int c = tid; c < a.chunks; c += kThreads) n += a.live[static_cast<size_t>(g) * a.chunks + c];
+                                                     static_cast<size_t>(g) * a.parts * EMAX);
+    const int words = a.parts * kQuads;
+    int n = tid < a.parts ? a.live[static_cast<size_t>(g) * a.parts + tid] : 0;
     int4 s = make_int4(0, 0, 0, 0);
     for (int b = tid; b < words; b += kFlight * kThreads) {
         int4 v[kFlight];
@@ -371,8 +395,8 @@ __device__ __forceinline__ void group_counts(const LossArgs& a, int g, int* tota
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
-    if (lane < kQuads) *reinterpret_cast<int4*>(&part[wave][lane * 4]) = s;
     if (lane == 0) part_n[wave] = n;
+    if (lane < kQuads) *reinterpret_cast<int4*>(&part[wave][lane * 4]) = s;
     __syncthreads();
     n_live = 0;
 #pragma unroll
@@ -386,52 +410,72 @@ __device__ __forceinline__ void group_counts(const LossArgs& a, int g, int* tota
     __syncthreads();
 }
 
-// Second pass: a chunk's rows, or (the block after a group's chunks) its losses.
-template <int EMAX>
-__global__ __launch_bounds__(64 * kChunkWaves) void gate_grad_kernel(LossArgs a) {
-    using R = Rows<EMAX, kChunkWaves>;
-    constexpr int kSlices = R::kThreads / EMAX;
-    __shared__ __align__(16) int total[EMAX];
-    __shared__ double part[R::kThreads];
+// A chunk's rows; where probs are read once, its sums.
+template <int EMAX, Pass PASS>
+__device__ __forceinline__ void chunk_rows(const LossArgs& a, int g, int chunk) {
+    __shared__ Sums<EMAX, kChunkWaves> sums;
+    __shared__ int total[EMAX];
+    const int tid = threadIdx.x;
+    const int t0 = chunk * a.chunk_tokens, t1 = min(t0 + a.chunk_tokens, a.Ng);
+    do_rows<EMAX, kChunkWaves, PASS>(a, static_cast<size_t>(g) * a.Ng, t0, t1, &sums,
+                                     [&](int e0, float (&f4)[4], float& per) {
+                                         int n_live;
+                                         group_counts<EMAX>(a, g, total, n_live);
+                                         shares(a, total, n_live, e0, f4, per);
+                                     });
+    if constexpr (PASS == kBoth) {
+        const size_t row = static_cast<size_t>(g) * a.chunks + chunk;
+        if (tid < EMAX) a.sum_p[row * EMAX + tid] = sums.prob(tid);
+        if (tid == 64) a.sum_z[row] = sums.square();
+    }
+}
+
+// A group's losses from its chunks' sums, by a block: four experts a lane,
+// kFlight rows of sums in flight.
+template <int EMAX, int kFlight>
+__device__ __forceinline__ void group_losses(const LossArgs& a, int g) {
+    constexpr int kThreads = 64 * kChunkWaves, kQuads = EMAX / 4, kSlices = kThreads / kQuads;
+    __shared__ int total[EMAX];
+    __shared__ double part[kChunkWaves][EMAX];
     __shared__ double sum_p[EMAX];
     __shared__ double part_z[kChunkWaves];
-    const int g = blockIdx.x / (a.chunks + 1), chunk = blockIdx.x % (a.chunks + 1);
-    const int tid = threadIdx.x;
-    int n_live;
-    if (chunk < a.chunks) {
-        const int t0 = chunk * a.chunk_tokens, t1 = min(t0 + a.chunk_tokens, a.Ng);
-        const size_t first = static_cast<size_t>(g) * a.Ng;
-        write_rows<EMAX, kChunkWaves>(
-            a, first, t0, t1, a.lse + first + t0, [&](float (&f4)[4], float& per) {
-                group_counts<EMAX>(a, g, total, n_live);
-                shares(a, total, n_live, ((tid & 63) % R::kLanes) * 4, f4, per);
-            });
-        return;
-    }
-    group_counts<EMAX>(a, g, total, n_live);
-    const int e = tid % EMAX, q = tid / EMAX;
-    const float* sp = a.sum_p + static_cast<size_t>(g) * a.chunks * EMAX + e;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = tid / kQuads;
+    const float4* sp = reinterpret_cast<const float4*>(
+                           a.sum_p + static_cast<size_t>(g) * a.chunks * EMAX) + tid % kQuads;
     const float* sz = a.sum_z + static_cast<size_t>(g) * a.chunks;
-    double s = 0.0, z = 0.0;
-    int c = q;
-    for (; c + 15 * kSlices < a.chunks; c += 16 * kSlices) {  // sixteen in flight, added in order
-        float v[16];
+    double s[4] = {0.0, 0.0, 0.0, 0.0}, z = 0.0;
+    for (int c = q; c < a.chunks; c += kFlight * kSlices) {
+        float4 v[kFlight];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) v[u] = sp[static_cast<size_t>(c + u * kSlices) * EMAX];
+        for (int u = 0; u < kFlight; ++u)
+            v[u] = c + u * kSlices < a.chunks ? sp[static_cast<size_t>(c + u * kSlices) * kQuads]
+                                              : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int u = 0; u < 16; ++u) s += v[u];
+        for (int u = 0; u < kFlight; ++u) {
+            s[0] += v[u].x;
+            s[1] += v[u].y;
+            s[2] += v[u].z;
+            s[3] += v[u].w;
+        }
     }
-    for (; c < a.chunks; c += kSlices) s += sp[static_cast<size_t>(c) * EMAX];
-    for (int i = tid; i < a.chunks; i += R::kThreads) z += sz[i];
+    for (int i = tid; i < a.chunks; i += kThreads) z += sz[i];
+    int n_live;
+    group_counts<EMAX>(a, g, total, n_live);
+#pragma unroll
+    for (int o = kQuads; o < 64; o <<= 1)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] += __shfl_xor(s[j], o);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
-    part[tid] = s;
-    if ((tid & 63) == 0) part_z[tid >> 6] = z;
+    if (lane < kQuads)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[wave][lane * 4 + j] = s[j];
+    if (lane == 0) part_z[wave] = z;
     __syncthreads();
     if (tid < EMAX) {
         double t = 0.0;
 #pragma unroll
-        for (int r = 0; r < kSlices; ++r) t += part[r * EMAX + tid];
+        for (int w = 0; w < kChunkWaves; ++w) t += part[w][tid];
         sum_p[tid] = t;
     }
     z = 0.0;
@@ -439,6 +483,25 @@ __global__ __launch_bounds__(64 * kChunkWaves) void gate_grad_kernel(LossArgs a)
     for (int w = 0; w < kChunkWaves; ++w) z += part_z[w];
     __syncthreads();
     write_losses(a, g, total, sum_p, z, n_live);
+}
+
+template <int EMAX>
+__global__ __launch_bounds__(64 * kChunkWaves) void gate_rows_kernel(LossArgs a) {
+    chunk_rows<EMAX, kBoth>(a, blockIdx.x / a.chunks, blockIdx.x % a.chunks);
+}
+
+template <int EMAX>
+__global__ __launch_bounds__(64 * kChunkWaves) void gate_losses_kernel(LossArgs a) {
+    group_losses<EMAX, 16>(a, blockIdx.x);
+}
+
+// Second launch of two: the block after a group's chunks writes its losses (with
+// few enough rows in flight not to cost the other blocks registers).
+template <int EMAX>
+__global__ __launch_bounds__(64 * kChunkWaves) void gate_gradient_kernel(LossArgs a) {
+    const int g = blockIdx.x / (a.chunks + 1), chunk = blockIdx.x % (a.chunks + 1);
+    if (chunk < a.chunks) chunk_rows<EMAX, kGradient>(a, g, chunk);
+    else group_losses<EMAX, 4>(a, g);
 }
 
 template <typename F>
@@ -451,25 +514,36 @@ void by_experts(int E, F f) {
 }
 
 struct Chunks {
-    int count, tokens, emax;
-    bool whole;  // a group in one block
+    int count, tokens;            // chunks of a group's rows
+    int parts, part_tokens;       // parts of its choices
+    int emax;
+    bool whole;                   // a group in one block
+    bool twice;                   // probs are read twice: parts are chunks
 };
 
-// Chunks of a group: about kBlocks over all groups, none shorter than a block's
-// step. More would cost every block of the second launch more rows of counts.
 Chunks chunks_of(const Dims& D) {
-    Chunks c = {1, 1, 4, false};
+    Chunks c = {1, 1, 1, 1, 4, false, false};
+    const auto split = [&](int most, int least_tokens, int& count, int& tokens) {
+        const int n = static_cast<int>(cdiv(D.Ng, least_tokens));
+        const int want = n < most ? n : most;
+        tokens = static_cast<int>(cdiv(D.Ng, want < 1 ? 1 : want));
+        if (tokens < 1) tokens = 1;
+        count = static_cast<int>(cdiv(D.Ng, tokens));
+        if (count < 1) count = 1;
+    };
     by_experts(D.E, [&](auto tag) {
         constexpr int EMAX = decltype(tag)::value;
         c.emax = EMAX;
         c.whole = D.Ng <= Rows<EMAX, kGroupWaves>::kGroupTokens;
-        const int most = static_cast<int>(cdiv(D.Ng, Rows<EMAX, kChunkWaves>::kBlockTokens));
-        int n = kBlocks / D.G;
-        if (n > kGroupChunks) n = kGroupChunks;
-        if (n > most) n = most;
-        if (n < 1) n = 1;
-        c.tokens = D.Ng > 0 ? static_cast<int>(cdiv(D.Ng, n)) : 1;
-        c.count = D.Ng > 0 ? static_cast<int>(cdiv(D.Ng, c.tokens)) : 1;
+        c.twice = static_cast<long long>(D.N) * D.E * 4 <= kRereadBytes;
+        int most = kBlocks / D.G;
+        if (c.twice && most > kGroupChunks) most = kGroupChunks;
+        split(most, Rows<EMAX, kChunkWaves>::kBlockTokens, c.count, c.tokens);
+        split(kGroupChunks, kCountTokens, c.parts, c.part_tokens);
+        if (c.twice) {
+            c.parts = c.count;
+            c.part_tokens = c.tokens;
+        }
     });
     return c;
 }
@@ -478,13 +552,14 @@ size_t pad16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
 
 }  // namespace
 
-// Workspace: lse [N], sums of probs and counts [G, chunks, EMAX], sums of lse^2
-// and numbers of tokens [G, chunks], each at a multiple of 16 bytes.
+// Workspace: sums of probs [G, chunks, EMAX], counts [G, parts, EMAX], sums of
+// lse^2 [G, chunks], numbers of tokens [G, parts] and, where probs are read
+// twice, lse [N], each at a multiple of 16 bytes.
 size_t gate_loss_workspace_bytes(const Dims& D) {
     const Chunks c = chunks_of(D);
-    const size_t rows = static_cast<size_t>(D.G) * c.count;
-    return pad16(sizeof(float) * static_cast<size_t>(D.N)) + 2 * sizeof(float) * rows * c.emax +
-           2 * pad16(sizeof(float) * rows);
+    const size_t rows = static_cast<size_t>(D.G) * c.count, parts = static_cast<size_t>(D.G) * c.parts;
+    return 4 * (rows + parts) * c.emax + pad16(4 * rows) + pad16(4 * parts) +
+           (c.twice ? pad16(4 * static_cast<size_t>(D.N)) : 0);
 }
 
 vmoe_status gate_loss_launch(const Dims& D, const float* logits, const float* bias,
@@ -493,11 +568,11 @@ vmoe_status gate_loss_launch(const Dims& D, const float* logits, const float* bi
                              int32_t* demand, float* mean_probs, float* dlogits, void* ws,
                              hipStream_t st) {
     const Chunks c = chunks_of(D);
-    const size_t rows = static_cast<size_t>(D.G) * c.count;
+    const size_t rows = static_cast<size_t>(D.G) * c.count, parts = static_cast<size_t>(D.G) * c.parts;
     unsigned char* w = static_cast<unsigned char*>(ws);
-    const auto take = [&w](size_t bytes) {
+    const auto take = [&w](size_t words) {
         unsigned char* p = w;
-        w += pad16(bytes);
+        w += pad16(4 * words);
         return p;
     };
     LossArgs a;
@@ -507,11 +582,11 @@ vmoe_status gate_loss_launch(const Dims& D, const float* logits, const float* bi
     a.probs = probs;
     a.idx = idx;
     a.mask = mask;
-    a.lse = reinterpret_cast<float*>(take(sizeof(float) * static_cast<size_t>(D.N)));
-    a.sum_p = reinterpret_cast<float*>(take(sizeof(float) * rows * c.emax));
-    a.counts = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * rows * c.emax));
-    a.sum_z = reinterpret_cast<float*>(take(sizeof(float) * rows));
-    a.live = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * rows));
+    a.sum_p = reinterpret_cast<float*>(take(rows * c.emax));
+    a.counts = reinterpret_cast<int32_t*>(take(parts * c.emax));
+    a.sum_z = reinterpret_cast<float*>(take(rows));
+    a.live = reinterpret_cast<int32_t*>(take(parts));
+    a.lse = c.twice ? reinterpret_cast<float*>(take(static_cast<size_t>(D.N))) : nullptr;
     a.losses = losses;
     a.mean_probs = mean_probs;
     a.dlogits = dlogits;
@@ -521,17 +596,25 @@ vmoe_status gate_loss_launch(const Dims& D, const float* logits, const float* bi
     a.k = D.k;
     a.chunks = c.count;
     a.chunk_tokens = c.tokens;
+    a.parts = c.parts;
+    a.part_tokens = c.part_tokens;
     a.w_balance = w_balance;
     a.w_z = w_z;
-    const unsigned grid = static_cast<unsigned>(rows);  // at most N or G
     by_experts(D.E, [&](auto tag) {
-        constexpr int EMAX = decltype(tag)::value;
+        constexpr int EMAX = decltype(tag)::value, kThreads = 64 * kChunkWaves;
         if (c.whole) {
             gate_group_kernel<EMAX><<<D.G, 64 * kGroupWaves, 0, st>>>(a);
             return;
         }
-        gate_sums_kernel<EMAX><<<grid, 64 * kChunkWaves, 0, st>>>(a);
-        gate_grad_kernel<EMAX><<<grid + D.G, 64 * kChunkWaves, 0, st>>>(a);
+        const unsigned blocks = static_cast<unsigned>(rows);  // at most N or G
+        if (c.twice) {
+            gate_count_kernel<EMAX, true><<<blocks, kThreads, 0, st>>>(a);
+            gate_gradient_kernel<EMAX><<<blocks + D.G, kThreads, 0, st>>>(a);
+            return;
+        }
+        gate_count_kernel<EMAX, false><<<static_cast<unsigned>(parts), kThreads, 0, st>>>(a);
+        gate_rows_kernel<EMAX><<<blocks, kThreads, 0, st>>>(a);
+        gate_losses_kernel<EMAX><<<D.G, kThreads, 0, st>>>(a);
     });
     return launch_status();
 }
