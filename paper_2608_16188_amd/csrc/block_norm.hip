@@ -495,57 +495,60 @@ struct ReduceArgs {
     int slot_w, slot_b, slot_s, slot_t, slots;
     int G, d, blocks_per_group, blocks;
     int tiles, jobs;  // column tiles; sums over all rows (the gate's blocks come after)
+    int slices;       // that share a group's rows
+    bool merged;      // dgate's blocks write dpost_weight and dpost_bias
 };
 
-// Blocks of 16 columns x 64 slices of the partial rows, one block a sum and
-// column tile, so that even a narrow model's sums fill some of the chip.
-constexpr int kReduceCols = 16, kSlices = 64;
-constexpr int kSmallGroup = 8;  // partial rows of a group that one thread adds
+// Blocks of 32 columns (a cache line of a partial row) x 32 slices of the rows,
+// one block a sum and column tile, so that even a narrow model's sums fill some
+// of the chip.
+constexpr int kReduceCols = 32, kSlices = 32;
+
+// Slices that share a group's partial rows in dgate's blocks.
+int group_slices(int rows) { return rows <= 8 ? 1 : rows <= 64 ? 8 : kSlices; }
 
 // Sum over rows first, first + stride, ... below end of a column, each times
-// its group's gate where there is one.
+// its group's gate where there is one; eight rows in flight, added in order.
 template <typename TA>
 __device__ __forceinline__ float column_sum(const float* p, size_t row, int first, int end,
                                             int stride, const TA* gate, int d, int per_group) {
     float s = 0.0f;
-    int r = first;
-    const auto weight = [&](int q) {
-        return gate ? Elem<TA>::load(gate, static_cast<size_t>(q / per_group) * d) : 1.0f;
-    };
-    for (; r + 7 * stride < end; r += 8 * stride) {  // eight rows in flight, added in order
+    for (int r = first; r < end; r += 8 * stride) {
         float v[8], w[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            v[u] = p[(r + u * stride) * row];
-            w[u] = weight(r + u * stride);
+            const int q = r + u * stride;
+            v[u] = q < end ? p[q * row] : 0.0f;
+            w[u] = gate && q < end
+                       ? Elem<TA>::load(gate, static_cast<size_t>(q / per_group) * d) : 1.0f;
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u) s = __builtin_fmaf(w[u], v[u], s);
     }
-    for (; r < end; r += stride) s = __builtin_fmaf(weight(r), p[r * row], s);
     return s;
 }
 
-// Adds the slices of each column in a fixed order, for the threads of slice 0.
-__device__ __forceinline__ float over_slices(float v, float (*lds)[kReduceCols]) {
-    v += __shfl_xor(v, 16);
-    v += __shfl_xor(v, 32);
+// Adds `slices` neighbouring slices of each column in order, for the threads of
+// the first of them.
+__device__ __forceinline__ float over_slices(float v, int slices, float (*lds)[kReduceCols]) {
+    const int c = threadIdx.x % kReduceCols, q = threadIdx.x / kReduceCols;
     __syncthreads();
-    if ((threadIdx.x & 63) < kReduceCols) lds[threadIdx.x / 64][threadIdx.x & 63] = v;
+    lds[q][c] = v;
     __syncthreads();
     float s = 0.0f;
-    if (threadIdx.x < kReduceCols)
-#pragma unroll
-        for (int q = 0; q < kSlices * kReduceCols / 64; ++q) s += lds[q][threadIdx.x];
+    if (q % slices == 0)
+        for (int k = 0; k < slices; ++k) s += lds[q + k][c];
     return s;
 }
 
 // Jobs: dpre_weight, dpre_bias, dpost_weight, dpost_bias (those asked for; the
-// last two weigh each partial row with its group's gate), then dgate, a block a
-// group and column tile, or 64 groups where a group has few partial rows.
+// last two weigh each partial row with its group's gate), then dgate, a block
+// as many groups and a column tile as its slices serve. The sums of an only
+// group give dpost_weight and dpost_bias too, without jobs of their own (and
+// with their bits: gate times the same sum).
 template <typename TA>
 __global__ __launch_bounds__(kReduceCols* kSlices) void block_norm_reduce_kernel(ReduceArgs a) {
-    __shared__ float lds[kSlices * kReduceCols / 64][kReduceCols];
+    __shared__ float lds[kSlices][kReduceCols];
     const int job = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
     const int c = tile * kReduceCols + threadIdx.x % kReduceCols, q = threadIdx.x / kReduceCols;
     const bool live = c < a.d;
@@ -555,34 +558,40 @@ __global__ __launch_bounds__(kReduceCols* kSlices) void block_norm_reduce_kernel
     const TA* gate = a.gate ? static_cast<const TA*>(a.gate) + cc : nullptr;
     if (job < a.jobs) {
         // the job-th of the sums that are asked for
-        float* const outs[4] = {a.dpre_w, a.dpre_b, a.dpost_w, a.dpost_b};
+        float* const outs[4] = {a.dpre_w, a.dpre_b, a.merged ? nullptr : a.dpost_w,
+                                a.merged ? nullptr : a.dpost_b};
         const int slots[4] = {a.slot_w, a.slot_b, a.slot_s, a.slot_t};
         int k = 0;
         for (int left = job; k < 4; ++k)
             if (outs[k] && left-- == 0) break;
-        const float s = over_slices(column_sum<TA>(column(slots[k]), row, q, a.blocks, kSlices,
-                                                   k >= 2 ? gate : nullptr, a.d,
-                                                   a.blocks_per_group), lds);
+        const bool weighted = k >= 2 && gate != nullptr;
+        float s = over_slices(column_sum<TA>(column(slots[k]), row, q, a.blocks, kSlices,
+                                             weighted && a.G > 1 ? gate : nullptr, a.d,
+                                             a.blocks_per_group), kSlices, lds);
+        if (weighted && a.G == 1) s *= Elem<TA>::load(gate, 0);
         if (q == 0 && live) outs[k][c] = s;
         return;
     }
     const float w = a.post_w ? Elem<TA>::load(static_cast<const TA*>(a.post_w), cc) : 1.0f;
     const float b = a.post_b ? Elem<TA>::load(static_cast<const TA*>(a.post_b), cc) : 0.0f;
-    const bool small = a.blocks_per_group <= kSmallGroup;
-    const int g = small ? (job - a.jobs) * kSlices + q : job - a.jobs;
-    if (small && g >= a.G) return;
-    const int first = g * a.blocks_per_group, end = first + a.blocks_per_group;
-    const int from = small ? first : first + q, stride = small ? 1 : kSlices;
-    float S = a.blocks ? column_sum<TA>(column(a.slot_s), row, from, end, stride, nullptr, 0, 1)
-                       : 0.0f;
-    float T = a.blocks && a.slot_t >= 0
-                  ? column_sum<TA>(column(a.slot_t), row, from, end, stride, nullptr, 0, 1) : 0.0f;
-    if (!small) {
-        S = over_slices(S, lds);
-        T = over_slices(T, lds);
-        if (q != 0) return;
+    const int g = (job - a.jobs) * (kSlices / a.slices) + q / a.slices, slice = q % a.slices;
+    const bool on = g < a.G && a.blocks > 0;
+    const int first = g * a.blocks_per_group, end = on ? first + a.blocks_per_group : first;
+    float S = column_sum<TA>(column(a.slot_s), row, first + slice, end, a.slices, nullptr, 0, 1);
+    float T = 0.0f;
+    if (a.slot_t >= 0)
+        T = column_sum<TA>(column(a.slot_t), row, first + slice, end, a.slices, nullptr, 0, 1);
+    if (a.slices > 1) {
+        S = over_slices(S, a.slices, lds);
+        T = over_slices(T, a.slices, lds);
     }
-    if (live) a.dgate[static_cast<size_t>(g) * a.d + c] = __builtin_fmaf(w, S, b * T);
+    if (!live || slice != 0 || g >= a.G) return;
+    a.dgate[static_cast<size_t>(g) * a.d + c] = __builtin_fmaf(w, S, b * T);
+    if (a.merged) {
+        const float gc = gate ? Elem<TA>::load(gate, 0) : 1.0f;
+        if (a.dpost_w) a.dpost_w[c] = gc * S;
+        if (a.dpost_b) a.dpost_b[c] = gc * T;
+    }
 }
 
 // Waves a row and steps a lane by width: one wave up to 1024 columns (no
@@ -705,15 +714,15 @@ vmoe_status block_norm_bwd_launch(const vmoe_norm_shape& s, const void* dx_out, 
     }
     if (slots > 0) {
         const int tiles = static_cast<int>(cdiv(s.d_model, kReduceCols));
-        const int jobs = (dpre_w != nullptr) + (dpre_b != nullptr) + (dpost_w != nullptr) +
-                         (dpost_b != nullptr);
-        const int gates = !dgate ? 0 : b.blocks_per_group <= kSmallGroup
-                                           ? static_cast<int>(cdiv(s.n_groups, kSlices))
-                                           : s.n_groups;
+        const bool merged = dgate && s.n_groups == 1;
+        const int jobs = (dpre_w != nullptr) + (dpre_b != nullptr) +
+                         (merged ? 0 : (dpost_w != nullptr) + (dpost_b != nullptr));
+        const int slices = s.n_groups == 1 ? kSlices : group_slices(b.blocks_per_group);
+        const int gates = dgate ? static_cast<int>(cdiv(s.n_groups, kSlices / slices)) : 0;
         const ReduceArgs r = {static_cast<float*>(ws), post_w, post_b, gate, dpre_w, dpre_b,
                               dpost_w, dpost_b, dgate, slot_w, slot_b, slot_s, slot_t, slots,
                               s.n_groups, s.d_model, b.blocks_per_group,
-                              static_cast<int>(b.blocks), tiles, jobs};
+                              static_cast<int>(b.blocks), tiles, jobs, slices, merged};
         const unsigned grid = static_cast<unsigned>(tiles) * static_cast<unsigned>(jobs + gates);
         if (s.dtype == VMOE_F32)
             block_norm_reduce_kernel<float><<<grid, kReduceCols * kSlices, 0, st>>>(r);
