@@ -349,8 +349,15 @@ __global__ __launch_bounds__(kThreads) void norm_final_kernel(const double* __re
                                                               float max_norm,
                                                               float* __restrict__ clip) {
     __shared__ double lds[kThreads / 64];
-    double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += kThreads) s += partial[i];
+    constexpr int U = kNormBlocks / kThreads;
+    double v[U], s = 0.0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = u * kThreads + threadIdx.x;
+        v[u] = i < n ? partial[i] : 0.0;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += v[u];
     s = block_sum(s, lds);
     if (threadIdx.x == 0) {
         const float norm = static_cast<float>(sqrt(s)) * fabsf(grad_scale);
@@ -360,7 +367,8 @@ __global__ __launch_bounds__(kThreads) void norm_final_kernel(const double* __re
     }
 }
 
-// Codes to values, 8 a lane and step.
+// Codes to values: 8 consecutive ones a lane and step (a store of 16 bytes of
+// bf16), all of a block's codes requested before any is used.
 template <typename T, bool SIGNED>
 __global__ __launch_bounds__(kThreads) void state_values_kernel(const uint8_t* __restrict__ codes,
                                                                 const uint8_t* __restrict__ scale,
@@ -371,22 +379,33 @@ __global__ __launch_bounds__(kThreads) void state_values_kernel(const uint8_t* _
     const uint8_t* s = scale + base / kStateBlock;
     T* o = out + base;
     constexpr bool BF16 = sizeof(T) == 2;
-    constexpr int U = VMOE_ADAMW_CHUNK / kSpan;
-    uint32_t w[U];
+    constexpr int U = VMOE_ADAMW_CHUNK / (2 * kSpan);
+    uint32_t w[U][2];
     int e[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int i = u * kSpan + threadIdx.x * kPer;
-        w[u] = load_codes<true>(c, i, count);
+        const int i = (u * kThreads + threadIdx.x) * 2 * kPer;
+        w[u][0] = load_codes<true>(c, i, count);
+        w[u][1] = load_codes<true>(c, i + kPer, count);
         e[u] = i < count ? s[i / kStateBlock] : 0;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int i = u * kSpan + threadIdx.x * kPer;
-        Four v;
+        const int i = (u * kThreads + threadIdx.x) * 2 * kPer;
+        Four v[2];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) v.x[j] = decode<SIGNED>(w[u] >> (8 * j), e[u]);
-        store4<true, BF16>(o, i, count, v);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[h].x[j] = decode<SIGNED>(w[u][h] >> (8 * j), e[u]);
+        if (BF16 && i + 2 * kPer <= count) {
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+            const u32x4 q = {pack_bf16x2(v[0].x[0], v[0].x[1]), pack_bf16x2(v[0].x[2], v[0].x[3]),
+                             pack_bf16x2(v[1].x[0], v[1].x[1]), pack_bf16x2(v[1].x[2], v[1].x[3])};
+            __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(o + i));
+        } else {
+            store4<true, BF16>(o, i, count, v[0]);
+            store4<true, BF16>(o, i + kPer, count, v[1]);
+        }
     }
 }
 

@@ -69,6 +69,7 @@ template <int W, int V>
 struct Team {
     static constexpr int kBlock = W == 1 ? 256 : W * kLanes;
     static constexpr int kRows = kBlock / (W * kLanes);  // rows a block works on at a time
+    static constexpr int kCols = W * kLanes * V * 8;
     // whether a row is requested while the one before it is worked on: a block
     // of 16 waves has no registers left for it
     static constexpr bool kAhead = W < 16;
@@ -298,26 +299,18 @@ struct BwdArgs {
     float residual, branch;
 };
 
-// One block's sums of one kind into its row of partials.
+// One sum of a block into its row of partials: a team of several waves writes its
+// columns, teams of one wave meet in LDS first.
 template <int W, int V>
-__device__ __forceinline__ void leave_sums(const float (&acc)[V][8], float* out, int d,
-                                           const int (&col)[V], float* lds) {
+__device__ __forceinline__ void leave_sum(const float (&acc)[V][8], float* out, int d,
+                                          const int (&col)[V], float* lds) {
     using T = Team<W, V>;
-    if constexpr (W > 1) {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
+    for (int i = 0; i < V; ++i) {
+        if constexpr (W > 1) {
             if (col[i] < d) store8(out + col[i], acc[i]);
-    } else {
-        constexpr int kCols = V * kLanes * 8;
-        __syncthreads();  // the last use of lds
-#pragma unroll
-        for (int i = 0; i < V; ++i) store8(lds + T::row() * kCols + col[i], acc[i]);
-        __syncthreads();
-        for (int c = threadIdx.x; c < d; c += T::kBlock) {
-            float s = 0.0f;
-#pragma unroll
-            for (int r = 0; r < T::kRows; ++r) s += lds[r * kCols + c];
-            out[c] = s;
+        } else {
+            store8(lds + T::row() * T::kCols + col[i], acc[i]);
         }
     }
 }
@@ -357,7 +350,9 @@ struct BwdRow {
 template <typename TS, typename TA, typename TH, int W, int V, bool POST>
 __global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_bwd_kernel(BwdArgs a) {
     using T = Team<W, V>;
-    __shared__ __align__(16) float lds[W == 1 ? T::kRows * V * kLanes * 8 : 4 * W];
+    // teams of one wave: their sums at the end, up to four kinds at once
+    constexpr int kSums = T::kRows * T::kCols;
+    __shared__ __align__(16) float lds[W == 1 ? (POST ? 4 : 3) * kSums : 4 * W];
     int turn = 0;
     int col[V];
 #pragma unroll
@@ -481,11 +476,23 @@ __global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_bwd_kernel(Bw
     if (a.slots == 0) return;
     float* out = a.partial + static_cast<size_t>(blockIdx.x) * a.slots * a.d;
     const auto slot = [&](int k) { return out + static_cast<size_t>(k) * a.d; };
-    if (a.slot_w >= 0) leave_sums<W, V>(acc_w, slot(a.slot_w), a.d, col, lds);
-    if (a.slot_b >= 0) leave_sums<W, V>(acc_b, slot(a.slot_b), a.d, col, lds);
-    if (a.slot_s >= 0) leave_sums<W, V>(acc_s, slot(a.slot_s), a.d, col, lds);
+    const auto shared = [&](int k) { return lds + (W == 1 ? k * kSums : 0); };
+    if (a.slot_w >= 0) leave_sum<W, V>(acc_w, slot(a.slot_w), a.d, col, shared(a.slot_w));
+    if (a.slot_b >= 0) leave_sum<W, V>(acc_b, slot(a.slot_b), a.d, col, shared(a.slot_b));
+    if (a.slot_s >= 0) leave_sum<W, V>(acc_s, slot(a.slot_s), a.d, col, shared(a.slot_s));
     if constexpr (POST)
-        if (a.slot_t >= 0) leave_sums<W, V>(acc_t, slot(a.slot_t), a.d, col, lds);
+        if (a.slot_t >= 0) leave_sum<W, V>(acc_t, slot(a.slot_t), a.d, col, shared(a.slot_t));
+    if constexpr (W == 1) {
+        __syncthreads();
+        for (int k = 0; k < a.slots; ++k)
+            for (int c = threadIdx.x * 4; c < a.d; c += T::kBlock * 4) {
+                f32x4 s = 0.0f;
+#pragma unroll
+                for (int r = 0; r < T::kRows; ++r)
+                    s += *reinterpret_cast<const f32x4*>(shared(k) + r * T::kCols + c);
+                *reinterpret_cast<f32x4*>(slot(k) + c) = s;
+            }
+    }
 }
 
 struct ReduceArgs {
