@@ -64,32 +64,58 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
 }
 
-// W waves a row, V steps of 8 columns a lane: columns (i W 64 + lane of team) 8.
-template <int W, int V>
+// A row's team: W waves, or L lanes of one; V steps of 8 columns a lane, columns
+// (i W L + lane of team) 8.
+template <int L, int W, int V>
 struct Team {
+    static_assert(L == kLanes || W == 1, "part of a wave, or whole waves");
+    static constexpr int kL = L, kW = W, kV = V;
     static constexpr int kBlock = W == 1 ? 256 : W * kLanes;
-    static constexpr int kRows = kBlock / (W * kLanes);  // rows a block works on at a time
-    static constexpr int kCols = W * kLanes * V * 8;
+    static constexpr int kRows = kBlock / (W * L);  // rows a block works on at a time
+    static constexpr int kCols = W * L * V * 8;
     // whether a row is requested while the one before it is worked on: a block
     // of 16 waves has no registers left for it
     static constexpr bool kAhead = W < 16;
     static __device__ __forceinline__ int lane() {
-        return W == 1 ? threadIdx.x & (kLanes - 1) : threadIdx.x;
+        return W == 1 ? threadIdx.x & (L - 1) : threadIdx.x;
     }
-    // the same in all lanes of a wave, and known to be: row addresses stay scalar
+    // of a whole wave: the same in all lanes, and known to be, so that row
+    // addresses stay scalar
     static __device__ __forceinline__ int row() {
-        return W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes) : 0;
+        if (W > 1) return 0;
+        return L == kLanes ? __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes)
+                           : threadIdx.x / L;
     }
-    static __device__ __forceinline__ int column(int i) { return (i * W * kLanes + lane()) * 8; }
+    static __device__ __forceinline__ int column(int i) { return (i * W * L + lane()) * 8; }
 };
+
+template <int CTRL>
+__device__ __forceinline__ float add_rotated(float v) {
+    const int x = __builtin_bit_cast(int, v);
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, CTRL, 0xF, 0xF, false));
+}
+
+// Sum over L lanes for all of them; lanes of one team are active together.
+template <int L>
+__device__ __forceinline__ float lanes_total(float v) {
+    if constexpr (L == kLanes) return wave_total(v);
+    v = add_rotated<0x128>(v);  // rotations within 16 lanes by 8, 4, 2, 1
+    v = add_rotated<0x124>(v);
+    v = add_rotated<0x122>(v);
+    v = add_rotated<0x121>(v);
+    if constexpr (L == 32)      // lane ^ 16
+        v += __builtin_bit_cast(
+            float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401F));
+    return v;
+}
 
 // Sums over a team, for every lane. The two halves of `lds` take turns, so one
 // barrier a call is enough: a half is written again only after the barrier of
 // the call between, which every wave passes after its reads.
-template <int W, int K>
+template <int L, int W, int K>
 __device__ __forceinline__ void team_sum(float (&s)[K], float* lds, int& turn) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) s[k] = wave_total(s[k]);
+    for (int k = 0; k < K; ++k) s[k] = lanes_total<L>(s[k]);
     if constexpr (W > 1) {
         float* half = lds + turn * 2 * W;
         turn ^= 1;
@@ -119,10 +145,10 @@ struct FwdArgs {
 
 // mean and 1/deviation of a row in registers. Columns past d hold 0 and are
 // left out of the sum about the mean.
-template <int W, int V>
+template <int L, int W, int V>
 __device__ __forceinline__ float2 row_stats(const float (&v)[V][8], int kind, int d, float eps,
                                             float inv_d, float* lds, int& turn) {
-    using T = Team<W, V>;
+    using T = Team<L, W, V>;
     float mean = 0.0f, s[1];
     if (kind == VMOE_NORM_LAYER) {
         s[0] = 0.0f;
@@ -130,7 +156,7 @@ __device__ __forceinline__ float2 row_stats(const float (&v)[V][8], int kind, in
         for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[0] += v[i][j];
-        team_sum<W, 1>(s, lds, turn);
+        team_sum<L, W, 1>(s, lds, turn);
         mean = s[0] * inv_d;
     }
     s[0] = 0.0f;
@@ -143,7 +169,7 @@ __device__ __forceinline__ float2 row_stats(const float (&v)[V][8], int kind, in
                 s[0] = __builtin_fmaf(c, c, s[0]);
             }
     }
-    team_sum<W, 1>(s, lds, turn);
+    team_sum<L, W, 1>(s, lds, turn);
     return make_float2(mean, 1.0f / sqrtf(__builtin_fmaf(s[0], inv_d, eps)));
 }
 
@@ -186,9 +212,9 @@ struct FwdRow {
 };
 
 // POST: whether the block's output has a norm.
-template <typename TS, typename TA, int W, int V, bool POST>
-__global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_fwd_kernel(FwdArgs a) {
-    using T = Team<W, V>;
+template <typename TS, typename TA, int L, int W, int V, bool POST>
+__global__ __launch_bounds__((Team<L, W, V>::kBlock)) void block_norm_fwd_kernel(FwdArgs a) {
+    using T = Team<L, W, V>;
     __shared__ float lds[4 * W];
     int turn = 0;
     int col[V];
@@ -228,7 +254,7 @@ __global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_fwd_kernel(Fw
             if constexpr (POST) {
                 float2 st = make_float2(0.0f, 0.0f);
                 if (on) {
-                    st = row_stats<W, V>(v, a.post, a.d, a.eps, inv_d, lds, turn);
+                    st = row_stats<L, W, V>(v, a.post, a.d, a.eps, inv_d, lds, turn);
 #pragma unroll
                     for (int i = 0; i < V; ++i)
 #pragma unroll
@@ -268,7 +294,7 @@ __global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_fwd_kernel(Fw
 #pragma unroll
                         for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
             }
-            const float2 st = row_stats<W, V>(v, a.pre, a.d, a.eps, inv_d, lds, turn);
+            const float2 st = row_stats<L, W, V>(v, a.pre, a.d, a.eps, inv_d, lds, turn);
             if (T::lane() == 0) reinterpret_cast<float2*>(a.pre_stats)[t] = st;
             TA* h = static_cast<TA*>(a.h) + at;
 #pragma unroll
@@ -301,10 +327,10 @@ struct BwdArgs {
 
 // One sum of a block into its row of partials: a team of several waves writes its
 // columns, teams of one wave meet in LDS first.
-template <int W, int V>
+template <int L, int W, int V>
 __device__ __forceinline__ void leave_sum(const float (&acc)[V][8], float* out, int d,
                                           const int (&col)[V], float* lds) {
-    using T = Team<W, V>;
+    using T = Team<L, W, V>;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         if constexpr (W > 1) {
@@ -347,9 +373,9 @@ struct BwdRow {
 
 // POST: whether the block's output has a norm. Without one there is no T to sum
 // (no bias) and no sum over the row on y's side.
-template <typename TS, typename TA, typename TH, int W, int V, bool POST>
-__global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_bwd_kernel(BwdArgs a) {
-    using T = Team<W, V>;
+template <typename TS, typename TA, typename TH, int L, int W, int V, bool POST>
+__global__ __launch_bounds__((Team<L, W, V>::kBlock)) void block_norm_bwd_kernel(BwdArgs a) {
+    using T = Team<L, W, V>;
     // teams of one wave: their sums at the end, up to four kinds at once
     constexpr int kSums = T::kRows * T::kCols;
     __shared__ __align__(16) float lds[W == 1 ? (POST ? 4 : 3) * kSums : 4 * W];
@@ -408,7 +434,7 @@ __global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_bwd_kernel(Bw
                     s[0] += dn;
                     s[1] = __builtin_fmaf(dn, n, s[1]);
                 }
-            team_sum<W, 2>(s, lds, turn);
+            team_sum<L, W, 2>(s, lds, turn);
             const float c0 = a.pre == VMOE_NORM_LAYER ? s[0] * inv_d : 0.0f, c1 = s[1] * inv_d;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -452,7 +478,7 @@ __global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_bwd_kernel(Bw
                     G[i][j] = dn;
                 }
             if constexpr (POST) {
-                team_sum<W, 2>(s, lds, turn);
+                team_sum<L, W, 2>(s, lds, turn);
                 const float c0 = a.post == VMOE_NORM_LAYER ? s[0] * inv_d : 0.0f, c1 = s[1] * inv_d;
 #pragma unroll
                 for (int i = 0; i < V; ++i)
@@ -477,11 +503,11 @@ __global__ __launch_bounds__((Team<W, V>::kBlock)) void block_norm_bwd_kernel(Bw
     float* out = a.partial + static_cast<size_t>(blockIdx.x) * a.slots * a.d;
     const auto slot = [&](int k) { return out + static_cast<size_t>(k) * a.d; };
     const auto shared = [&](int k) { return lds + (W == 1 ? k * kSums : 0); };
-    if (a.slot_w >= 0) leave_sum<W, V>(acc_w, slot(a.slot_w), a.d, col, shared(a.slot_w));
-    if (a.slot_b >= 0) leave_sum<W, V>(acc_b, slot(a.slot_b), a.d, col, shared(a.slot_b));
-    if (a.slot_s >= 0) leave_sum<W, V>(acc_s, slot(a.slot_s), a.d, col, shared(a.slot_s));
+    if (a.slot_w >= 0) leave_sum<L, W, V>(acc_w, slot(a.slot_w), a.d, col, shared(a.slot_w));
+    if (a.slot_b >= 0) leave_sum<L, W, V>(acc_b, slot(a.slot_b), a.d, col, shared(a.slot_b));
+    if (a.slot_s >= 0) leave_sum<L, W, V>(acc_s, slot(a.slot_s), a.d, col, shared(a.slot_s));
     if constexpr (POST)
-        if (a.slot_t >= 0) leave_sum<W, V>(acc_t, slot(a.slot_t), a.d, col, shared(a.slot_t));
+        if (a.slot_t >= 0) leave_sum<L, W, V>(acc_t, slot(a.slot_t), a.d, col, shared(a.slot_t));
     if constexpr (W == 1) {
         __syncthreads();
         for (int k = 0; k < a.slots; ++k)
@@ -601,20 +627,22 @@ __global__ __launch_bounds__(kReduceCols* kSlices) void block_norm_reduce_kernel
     }
 }
 
-// Waves a row and steps a lane by width: one wave up to 1024 columns (no
+// Lanes or waves a row and steps a lane by width: as few lanes as hold it up to 512
+// columns (39603 rows of 72 take 16 us backward, 29 with a wave a row), one wave up to 1024 (no
 // barrier in a row: 25216 rows of 768 take 45 us backward, 60 with two waves a
 // row), more waves beyond, so that the backward's sums and two rows stay in
 // registers (8197 rows of 4096: 122 us with eight waves, 128 with four; 4000 of
 // 8192: 105 with eight, 110 with sixteen).
 template <typename F>
 void by_width(int d, F f) {
-    using std::integral_constant;
-    if (d <= 512) f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    else if (d <= 1024) f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-    else if (d <= 2048) f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    else if (d <= 4096) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    else if (d <= 8192) f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
-    else f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    if (d <= 128) f(Team<16, 1, 1>{});
+    else if (d <= 256) f(Team<32, 1, 1>{});
+    else if (d <= 512) f(Team<64, 1, 1>{});
+    else if (d <= 1024) f(Team<64, 1, 2>{});
+    else if (d <= 2048) f(Team<64, 4, 1>{});
+    else if (d <= 4096) f(Team<64, 8, 1>{});
+    else if (d <= 8192) f(Team<64, 8, 2>{});
+    else f(Team<64, 16, 2>{});
 }
 
 template <typename F>
@@ -634,7 +662,8 @@ struct BwdGrid {
 BwdGrid bwd_grid(const vmoe_norm_shape& s) {
     const int Ng = s.n_tokens / s.n_groups;
     if (Ng == 0) return {1, 1, 0};
-    const int least = s.d_model <= 1024 ? 4 : 1;
+    int least = 1;
+    by_width(s.d_model, [&](auto team) { least = decltype(team)::kRows; });
     int per_group = (s.d_model <= 2048 ? 512 : 256) / s.n_groups;
     const int most = (Ng + least - 1) / least;
     if (per_group > most) per_group = most;
@@ -661,20 +690,20 @@ vmoe_status block_norm_fwd_launch(const vmoe_norm_shape& s, const void* x, const
     const FwdArgs a = {x, y, post_w, post_b, gate, row_scale, pre_w, pre_b, x_out, h, post_stats,
                        pre_stats, s.n_tokens, s.n_tokens / s.n_groups, s.n_groups, s.d_model,
                        s.pre_norm, s.post_norm, s.eps, s.residual_scale, s.branch_scale};
-    by_width(s.d_model, [&](auto wt, auto vt) {
-        constexpr int W = decltype(wt)::value, V = decltype(vt)::value;
-        using T = Team<W, V>;
+    by_width(s.d_model, [&](auto team) {
+        using T = decltype(team);
+        constexpr int L = T::kL, W = T::kW, V = T::kV;
         // as many waves as stay resident, each on several rows
         const unsigned rows = cdiv(s.n_tokens, T::kRows), most = 4096 * kLanes / T::kBlock;
         const unsigned grid = rows < most ? rows : most;
         by_flag(s.post_norm != VMOE_NORM_NONE, [&](auto post) {
             constexpr bool P = decltype(post)::value;
             if (s.dtype == VMOE_F32)
-                block_norm_fwd_kernel<float, float, W, V, P><<<grid, T::kBlock, 0, st>>>(a);
+                block_norm_fwd_kernel<float, float, L, W, V, P><<<grid, T::kBlock, 0, st>>>(a);
             else if (s.stream_dtype == VMOE_F32)
-                block_norm_fwd_kernel<float, uint16_t, W, V, P><<<grid, T::kBlock, 0, st>>>(a);
+                block_norm_fwd_kernel<float, uint16_t, L, W, V, P><<<grid, T::kBlock, 0, st>>>(a);
             else
-                block_norm_fwd_kernel<uint16_t, uint16_t, W, V, P><<<grid, T::kBlock, 0, st>>>(a);
+                block_norm_fwd_kernel<uint16_t, uint16_t, L, W, V, P><<<grid, T::kBlock, 0, st>>>(a);
         });
     });
     return launch_status();
@@ -699,23 +728,23 @@ vmoe_status block_norm_bwd_launch(const vmoe_norm_shape& s, const void* dx_out, 
                        s.branch_scale};
     if (b.blocks > 0) {
         const unsigned grid = static_cast<unsigned>(b.blocks);
-        by_width(s.d_model, [&](auto wt, auto vt) {
-            constexpr int W = decltype(wt)::value, V = decltype(vt)::value;
-            constexpr int B = Team<W, V>::kBlock;
+        by_width(s.d_model, [&](auto team) {
+            using T = decltype(team);
+            constexpr int L = T::kL, W = T::kW, V = T::kV, B = T::kBlock;
             const bool h32 = s.dh_dtype == VMOE_F32;
             by_flag(s.post_norm != VMOE_NORM_NONE, [&](auto post) {
                 constexpr bool P = decltype(post)::value;
                 using B16 = uint16_t;
                 if (s.dtype == VMOE_F32)
-                    block_norm_bwd_kernel<float, float, float, W, V, P><<<grid, B, 0, st>>>(a);
+                    block_norm_bwd_kernel<float, float, float, L, W, V, P><<<grid, B, 0, st>>>(a);
                 else if (s.stream_dtype == VMOE_F32 && h32)
-                    block_norm_bwd_kernel<float, B16, float, W, V, P><<<grid, B, 0, st>>>(a);
+                    block_norm_bwd_kernel<float, B16, float, L, W, V, P><<<grid, B, 0, st>>>(a);
                 else if (s.stream_dtype == VMOE_F32)
-                    block_norm_bwd_kernel<float, B16, B16, W, V, P><<<grid, B, 0, st>>>(a);
+                    block_norm_bwd_kernel<float, B16, B16, L, W, V, P><<<grid, B, 0, st>>>(a);
                 else if (h32)
-                    block_norm_bwd_kernel<B16, B16, float, W, V, P><<<grid, B, 0, st>>>(a);
+                    block_norm_bwd_kernel<B16, B16, float, L, W, V, P><<<grid, B, 0, st>>>(a);
                 else
-                    block_norm_bwd_kernel<B16, B16, B16, W, V, P><<<grid, B, 0, st>>>(a);
+                    block_norm_bwd_kernel<B16, B16, B16, L, W, V, P><<<grid, B, 0, st>>>(a);
             });
         });
     }
