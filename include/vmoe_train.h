@@ -235,7 +235,8 @@ vmoe_status vmoe_adamw(const void* plan, int64_t n_chunks, const vmoe_adamw_hype
 
 /* The values of an 8-bit state (checkpoints, inspection): out [n] out_dtype; both
  * types hold them exactly unless they leave the normal range. is_signed: 1 for
- * m, 0 for v. codes [n] u8 4-byte aligned, scale [ceil(n / 128)] u8. */
+ * m, 0 for v. codes [n] u8 4-byte aligned, scale [ceil(n / 128)] u8; n of 2^36
+ * and more is VMOE_ERR_UNSUPPORTED. */
 vmoe_status vmoe_adamw_state_values(const uint8_t* codes, const uint8_t* scale, int32_t is_signed,
                                     int64_t n, void* out, int32_t out_dtype, void* stream);
 

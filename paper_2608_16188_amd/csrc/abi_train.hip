@@ -40,7 +40,7 @@ namespace {
 
 constexpr int kMaxNormWidth = 16384;
 constexpr long long kMaxChunks = 0x7FFFFFFFLL;
-constexpr long long kMaxValueChunks = 1LL << 24;  // 2^32 threads of a launch, 256 a chunk
+constexpr long long kMaxValues = 1LL << 36;  // a launch has fewer than 2^32 threads
 
 bool known_dtype(int t) { return t == VMOE_F32 || t == VMOE_BF16; }
 bool known_norm(int k) { return k >= VMOE_NORM_NONE && k <= VMOE_NORM_LAYER; }
@@ -208,7 +208,7 @@ vmoe_status vmoe_adamw_state_values(const uint8_t* codes, const uint8_t* scale, 
     VMOE_TRY(need(n >= 0 && (is_signed == 0 || is_signed == 1) && known_dtype(out_dtype)));
     VMOE_TRY(need(n == 0 || (codes && (reinterpret_cast<uintptr_t>(codes) & 3u) == 0 && scale &&
                              dev(out))));
-    if (n / VMOE_ADAMW_CHUNK >= kMaxValueChunks) return VMOE_ERR_UNSUPPORTED;
+    if (n >= kMaxValues) return VMOE_ERR_UNSUPPORTED;
     return state_values_launch(codes, scale, is_signed == 1, n, out, out_dtype, as_stream(stream));
 }
 

@@ -23,7 +23,7 @@ constexpr int kSpan = kThreads * kPer;
 constexpr int kStepThreads = 128;  // of a block of the update
 constexpr int kStepSpan = kStepThreads * kPer;
 constexpr int kStateBlock = 128;  // elements of a scale byte, on 32 lanes
-constexpr int kNormBlocks = 2048;
+constexpr int kNormBlocks = 1024;
 
 enum : uint32_t { kParamBf16 = 1, kGradBf16 = 2, kState8 = 4 };
 
@@ -366,18 +366,21 @@ __global__ __launch_bounds__(kThreads) void norm_final_kernel(const double* __re
 }
 
 // Codes to values: 8 consecutive ones a lane and step (a store of 16 bytes of
-// bf16), all of a block's codes requested before any is used.
+// bf16), all of a block's codes requested before any is used (61.6 million to
+// bf16: 33 us, 5.5 TB/s; 35 with twice or half as many a block).
+constexpr int kValues = 4096;
+
 template <typename T, bool SIGNED>
 __global__ __launch_bounds__(kThreads) void state_values_kernel(const uint8_t* __restrict__ codes,
                                                                 const uint8_t* __restrict__ scale,
                                                                 long long n, T* __restrict__ out) {
-    const long long base = static_cast<long long>(blockIdx.x) * VMOE_ADAMW_CHUNK;
-    const int count = n - base < VMOE_ADAMW_CHUNK ? static_cast<int>(n - base) : VMOE_ADAMW_CHUNK;
+    const long long base = static_cast<long long>(blockIdx.x) * kValues;
+    const int count = n - base < kValues ? static_cast<int>(n - base) : kValues;
     const uint8_t* c = codes + base;
     const uint8_t* s = scale + base / kStateBlock;
     T* o = out + base;
     constexpr bool BF16 = sizeof(T) == 2;
-    constexpr int U = VMOE_ADAMW_CHUNK / (2 * kSpan);
+    constexpr int U = kValues / (2 * kSpan);
     uint32_t w[U][2];
     int e[U];
 #pragma unroll
@@ -518,7 +521,7 @@ vmoe_status adamw_launch(const void* plan, long long n_chunks, const vmoe_adamw_
 vmoe_status state_values_launch(const uint8_t* codes, const uint8_t* scale, bool is_signed,
                                 long long n, void* out, int out_dtype, hipStream_t st) {
     if (n == 0) return VMOE_OK;
-    const unsigned grid = static_cast<unsigned>(chunks_of(n));
+    const unsigned grid = cdiv(n, kValues);
     if (out_dtype == VMOE_BF16) {
         uint16_t* o = static_cast<uint16_t*>(out);
         if (is_signed)

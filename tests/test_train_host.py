@@ -288,3 +288,7 @@ def test_new_states():
     assert set(T.adamw_state(p.float())) == {"m", "v"}
     with pytest.raises(ValueError):
         T.adamw_state(p, bits=4)
+
+
+def test_values_of_too_long_states_refused():
+    assert call("vmoe_adamw_state_values", FAKE, FAKE, 1, 1 << 36, FAKE, 0, None) == UNS
