@@ -181,7 +181,9 @@ typedef struct vmoe_adamw_hyper {
     double lr;          /* finite, >= 0                                               */
     double beta1;       /* in [0, 1)                                                  */
     double beta2;       /* in [0, 1)                                                  */
-    double eps;         /* finite, at least 2^-126                                    */
+    double eps;         /* finite, at least 2^-126. Squares of gradients below some
+                           2^-75 are 0 in f32: with an eps below them, grad_scale has
+                           to bring gradients above that                              */
     double grad_scale;  /* finite: gradients are multiplied by it                     */
     int64_t step;       /* >= 1: this step's number, for the bias corrections         */
     uint32_t seed;      /* of the random numbers (with step and the element's number) */

@@ -229,8 +229,11 @@ __device__ __forceinline__ void adamw_span(const Entry& e, const Scalars& h, flo
         m.x[j] = mj;
         v.x[j] = vj;
         // the square root and the quotient to an ulp or two: their errors
-        // reach p below its own rounding, by a factor of lr
-        const float den = __builtin_fmaf(__builtin_amdgcn_sqrtf(vj), h.c2, h.eps);
+        // reach p below its own rounding, by a factor of lr. The instruction
+        // takes numbers below 2^-126 as 0: it gets them 2^32 times as large
+        const bool tiny = vj < 0x1p-126f;
+        const float root = __builtin_amdgcn_sqrtf(tiny ? vj * 0x1p32f : vj);
+        const float den = __builtin_fmaf(root, tiny ? h.c2 * 0x1p-16f : h.c2, h.eps);
         const float step = __builtin_fmaf(decay, p.x[j], (mj * h.c1) * __builtin_amdgcn_rcpf(den));
         p.x[j] = __builtin_fmaf(-lr, step, p.x[j]);
     }
