@@ -509,9 +509,13 @@ vmoe_status adamw_launch(const void* plan, long long n_chunks, const vmoe_adamw_
     h.b2 = static_cast<float>(hy.beta2);
     h.b2c = static_cast<float>(1.0 - hy.beta2);
     const double t = static_cast<double>(hy.step);
-    h.c1 = static_cast<float>(1.0 / (1.0 - pow(hy.beta1, t)));
-    h.c2 = static_cast<float>(1.0 / sqrt(1.0 - pow(hy.beta2, t)));
-    h.eps = static_cast<float>(hy.eps);
+    // m c1 / (sqrt(v) c2 + eps) with a large eps: both sides 2^-64 times as large,
+    // since the reciprocal of a number above 2^126 would be lost below the normal
+    // range (the root's side stays below 2^91, c2 being at most 2^27)
+    const double side = hy.eps >= 0x1p64 ? 0x1p-64 : 1.0;
+    h.c1 = static_cast<float>(side / (1.0 - pow(hy.beta1, t)));
+    h.c2 = static_cast<float>(side / sqrt(1.0 - pow(hy.beta2, t)));
+    h.eps = static_cast<float>(side * hy.eps);
     h.lr = static_cast<float>(hy.lr);
     h.grad_scale = static_cast<float>(hy.grad_scale);
     h.key = mix32(hy.seed ^ mix32(static_cast<uint32_t>(hy.step) * kGolden));

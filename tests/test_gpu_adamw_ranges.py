@@ -1,5 +1,5 @@
 """AdamW's weights where f32 runs out of range: second moments below 2^-126 with
-an eps as small.
+an eps as small, and an eps whose reciprocal is below it.
 
 m and v follow the text operation by operation, so they are given in f32
 arithmetic; the weights are the formula in float64 on those. Bound, U = 2^-24: a
@@ -76,3 +76,13 @@ def test_first_step_is_the_learning_rate():
     g = np.full(512, 2e-19, np.float32)
     up = check(g, np.zeros_like(g), np.zeros_like(g), 1e-30, 1, 32)
     assert np.abs(up - 1).max() < 1e-3  # v has some 13 bits
+
+
+@pytest.mark.parametrize("eps", [2.0 ** 100, 1e38, 3e38])
+def test_large_eps(eps):
+    """The reciprocal of a denominator above 2^126 is below the normal range."""
+    rng = np.random.default_rng(3)
+    n = 640
+    m0 = (rng.standard_normal(n) * 1e36).astype(np.float32)
+    v0 = np.ones(n, np.float32)
+    check(rng.standard_normal(n).astype(np.float32), m0, v0, eps, 3, 32)
