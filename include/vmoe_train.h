@@ -231,7 +231,9 @@ vmoe_status vmoe_grad_norm(const void* plan, int64_t n_chunks, double grad_scale
  * in f32, each product and sum of m and v rounded by itself (so that two
  * programs that follow this text get the same 8-bit states); p from the new
  * moments before they are rounded to 8 bits. p is master where there is one.
- * A clip[1] that is NaN leaves every tensor as it is. */
+ * A clip[1] that is NaN leaves every tensor as it is; no step was taken then, and
+ * the next call's step is to be the same number again, or its bias corrections
+ * assume a gradient that the moments have not seen. */
 vmoe_status vmoe_adamw(const void* plan, int64_t n_chunks, const vmoe_adamw_hyper* hyper,
                        const float* clip, void* stream);
 

@@ -7,11 +7,13 @@
 `SparseBlock` owns the stream, the norms' and the gate's parameters and their
 gradients beside the layer's `LayerBuffers`, all allocated once; `forward`,
 `backward` and `update` enqueue their calls on the current stream and allocate
-nothing. `python -m paper_2608_16188_amd.block` trains one on a fixed target.
+nothing; `update` also waits for the update before it, to learn whether that one
+was skipped. `python -m paper_2608_16188_amd.block` trains one on a fixed target.
 """
 from __future__ import annotations
 
 import argparse
+import contextlib
 import math
 import time
 
@@ -22,6 +24,14 @@ from . import workloads as W
 from .layer import LayerBuffers
 
 NORMS = {"none": T.VMOE_NORM_NONE, "rms": T.VMOE_NORM_RMS, "layer": T.VMOE_NORM_LAYER}
+
+
+def _current(stream):
+    """Context in which `stream` (None, a torch stream or a handle) is the current one."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream")
+                             else torch.cuda.ExternalStream(stream))
 
 
 class SparseBlock:
@@ -85,7 +95,23 @@ class SparseBlock:
             for k, p in self.params.items()], dev)
         self.clip = new(f32, 2)
         self.clip_ws = ws(T.vmoe_grad_norm_workspace_bytes(self.plan))
-        self.steps = 0
+        self._steps = 0  # but for the last update, until its clip is on the host
+        self._clip_host = torch.empty(2, pin_memory=True)
+        self._clip_there, self._clip_pending = torch.cuda.Event(), False
+
+    @property
+    def steps(self) -> int:
+        """Steps taken: updates but for those whose gradient norm was not finite,
+        which change nothing. Waits until the last one's norm is known."""
+        if self._clip_pending:
+            self._clip_there.synchronize()
+            self._clip_pending = False
+            self._steps += not math.isnan(self._clip_host[1])
+        return self._steps
+
+    @steps.setter
+    def steps(self, taken: int):
+        self._clip_pending, self._steps = False, taken
 
     def forward(self, stream=None):
         """From self.x to self.x_out and self.h_out."""
@@ -116,11 +142,15 @@ class SparseBlock:
 
     def update(self, lr: float, seed: int = 0, stream=None, **hyper):
         """One AdamW step on the gradients of the last backward, their norm held
-        to max_norm; hyper: beta1, beta2, eps."""
-        self.steps += 1
-        T.vmoe_grad_norm(self.plan, self.max_norm, self.clip, self.clip_ws, stream=stream)
-        T.vmoe_adamw(self.plan, lr, step=self.steps, seed=seed, clip=self.clip, stream=stream,
-                     **hyper)
+        to max_norm; hyper: beta1, beta2, eps. A norm that is not finite changes
+        nothing and is not counted."""
+        with _current(stream):
+            step = self.steps + 1
+            T.vmoe_grad_norm(self.plan, self.max_norm, self.clip, self.clip_ws)
+            T.vmoe_adamw(self.plan, lr, step=step, seed=seed, clip=self.clip, **hyper)
+            self._clip_host.copy_(self.clip, non_blocking=True)
+            self._clip_there.record()
+            self._clip_pending = True
 
 
 def train(cfg, inputs, target, steps, lr, report=None, **options):
