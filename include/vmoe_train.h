@@ -233,7 +233,11 @@ vmoe_status vmoe_grad_norm(const void* plan, int64_t n_chunks, double grad_scale
  * moments before they are rounded to 8 bits. p is master where there is one.
  * A clip[1] that is NaN leaves every tensor as it is; no step was taken then, and
  * the next call's step is to be the same number again, or its bias corrections
- * assume a gradient that the moments have not seen. */
+ * assume a gradient that the moments have not seen.
+ * hyper is read by the call: a graph that captured it repeats that step's number on
+ * every replay, so its rate and bias corrections stay and 8-bit states are rounded
+ * with the same random numbers each time, no longer free of bias. A training step's
+ * graph is to end before this call. */
 vmoe_status vmoe_adamw(const void* plan, int64_t n_chunks, const vmoe_adamw_hyper* hyper,
                        const float* clip, void* stream);
 

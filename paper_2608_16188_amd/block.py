@@ -143,8 +143,13 @@ class SparseBlock:
     def update(self, lr: float, seed: int = 0, stream=None, **hyper):
         """One AdamW step on the gradients of the last backward, their norm held
         to max_norm; hyper: beta1, beta2, eps. A norm that is not finite changes
-        nothing and is not counted."""
+        nothing and is not counted. Not to be captured in a graph (RuntimeError):
+        forward and backward are."""
         with _current(stream):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("update cannot be captured: a graph would repeat the step "
+                                   "number, and with it the learning rate, the bias corrections "
+                                   "and the random numbers of 8-bit states")
             step = self.steps + 1
             T.vmoe_grad_norm(self.plan, self.max_norm, self.clip, self.clip_ws)
             T.vmoe_adamw(self.plan, lr, step=step, seed=seed, clip=self.clip, **hyper)

@@ -72,3 +72,18 @@ def test_steps_can_be_set():
     go(b, up)
     assert (a.steps, b.steps) == (2, 41)
     assert not same_bits(a.params["w1"], b.params["w1"])
+
+
+def test_a_captured_update_is_refused():
+    """A replay would repeat the step number that was recorded."""
+    b = make(8)
+    go(b, torch.randn(96, 64, device="cuda"))
+    torch.cuda.synchronize()
+    before = {k: p.clone() for k, p in b.params.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.forward()
+        with pytest.raises(RuntimeError, match="captured"):
+            b.update(1e-3)
+    torch.cuda.synchronize()
+    assert b.steps == 1 and all(same_bits(b.params[k], p) for k, p in before.items())
