@@ -58,6 +58,7 @@ struct LossArgs {
     float *losses, *mean_probs, *dlogits;
     int32_t* demand;
     int Ng, E, k, chunks, chunk_tokens, parts, part_tokens;
+    int first_group;           // of a launch of whole groups
     float w_balance, w_z;
 };
 
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(64 * kGroupWaves) void gate_group_kernel(LossArgs a
     __shared__ Sums<EMAX, kGroupWaves> sums;
     __shared__ int total[EMAX];
     __shared__ double sum_p[EMAX];
-    const int g = blockIdx.x, tid = threadIdx.x;
+    const int g = a.first_group + blockIdx.x, tid = threadIdx.x;
     const size_t first = static_cast<size_t>(g) * a.Ng;
     int n_live = 0;
     const auto totals = [&] {
@@ -601,10 +602,17 @@ vmoe_status gate_loss_launch(const Dims& D, const float* logits, const float* bi
     a.part_tokens = c.part_tokens;
     a.w_balance = w_balance;
     a.w_z = w_z;
+    a.first_group = 0;
     by_experts(D.E, [&](auto tag) {
         constexpr int EMAX = decltype(tag)::value, kThreads = 64 * kChunkWaves;
         if (c.whole) {
-            gate_group_kernel<EMAX><<<D.G, 64 * kGroupWaves, 0, st>>>(a);
+            // a launch has fewer than 2^32 threads (groups too long for a block are
+            // never so many)
+            constexpr int kMost = 1 << 21;
+            for (a.first_group = 0; a.first_group < D.G; a.first_group += kMost) {
+                const int n = D.G - a.first_group < kMost ? D.G - a.first_group : kMost;
+                gate_group_kernel<EMAX><<<n, 64 * kGroupWaves, 0, st>>>(a);
+            }
             return;
         }
         const unsigned blocks = static_cast<unsigned>(rows);  // at most N or G

@@ -83,6 +83,12 @@ def test_groups_without_a_live_token(name):
         assert (got[k][1::2] == 0).all(), k
 
 
+def test_more_groups_than_a_launch_has_blocks():
+    c = Case((1 << 21) + 5, 1, 2, 1, True, False, 0.3, seed=8)
+    say("load balance", c.G, "groups")
+    check(c)
+
+
 def test_a_large_gate_from_a_graph():
     from paper_2608_16188_amd import vmoe_train as T
     c = make("e33_groups")
