@@ -25,6 +25,7 @@ namespace vmoe {
 namespace {
 
 constexpr int kLanes = 64;
+constexpr long long kMostThreads = 1LL << 31;  // of a launch, which takes fewer than 2^32
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -328,6 +329,7 @@ struct BwdArgs {
     int N, Ng, G, d, pre, post;
     int blocks_per_group, rows_per_block;
     float residual, branch;
+    int first_block;                 // of this launch
 };
 
 // One sum of a block into its row of partials: a team of several waves writes its
@@ -389,8 +391,8 @@ __global__ __launch_bounds__((Team<L, W, V>::kBlock)) void block_norm_bwd_kernel
 #pragma unroll
     for (int i = 0; i < V; ++i) col[i] = T::column(i);
     const float inv_d = 1.0f / static_cast<float>(a.d);
-    const int g = blockIdx.x / a.blocks_per_group;
-    const int part = blockIdx.x % a.blocks_per_group;
+    const int block = a.first_block + blockIdx.x;
+    const int g = block / a.blocks_per_group, part = block % a.blocks_per_group;
     const int t0 = g * a.Ng + part * a.rows_per_block;
     const int t1 = min(t0 + a.rows_per_block, (g + 1) * a.Ng);
     Raw8<TA> pre_w[V], post_w[V], gate[V];
@@ -505,7 +507,7 @@ __global__ __launch_bounds__((Team<L, W, V>::kBlock)) void block_norm_bwd_kernel
     }
 
     if (a.slots == 0) return;
-    float* out = a.partial + static_cast<size_t>(blockIdx.x) * a.slots * a.d;
+    float* out = a.partial + static_cast<size_t>(block) * a.slots * a.d;
     const auto slot = [&](int k) { return out + static_cast<size_t>(k) * a.d; };
     const auto shared = [&](int k) { return lds + (W == 1 ? k * kSums : 0); };
     if (a.slot_w >= 0) leave_sum<L, W, V>(acc_w, slot(a.slot_w), a.d, col, shared(a.slot_w));
@@ -535,6 +537,7 @@ struct ReduceArgs {
     int tiles, jobs;  // column tiles; sums over all rows (the gate's blocks come after)
     int slices;       // that share a group's rows
     bool merged;      // dgate's blocks write dpost_weight and dpost_bias
+    int first_job;    // of this launch
 };
 
 // Blocks of 32 columns (a cache line of a partial row) x 32 slices of the rows,
@@ -587,7 +590,7 @@ __device__ __forceinline__ float over_slices(float v, int slices, float (*lds)[k
 template <typename TA>
 __global__ __launch_bounds__(kReduceCols* kSlices) void block_norm_reduce_kernel(ReduceArgs a) {
     __shared__ float lds[kSlices][kReduceCols];
-    const int job = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
+    const int job = a.first_job + blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
     const int c = tile * kReduceCols + threadIdx.x % kReduceCols, q = threadIdx.x / kReduceCols;
     const bool live = c < a.d;
     const int cc = live ? c : 0;
@@ -654,6 +657,10 @@ template <typename F>
 void by_flag(bool on, F f) {
     if (on) f(std::true_type{});
     else f(std::false_type{});
+}
+
+unsigned at_most(long long n, long long most) {
+    return static_cast<unsigned>(n < most ? n : most);
 }
 
 struct BwdGrid {
@@ -731,17 +738,18 @@ vmoe_status block_norm_bwd_launch(const vmoe_norm_shape& s, const void* dx_out, 
     const int slot_w = dpre_w ? slots++ : -1, slot_b = dpre_b ? slots++ : -1;
     const int slot_s = dpost_w || dgate ? slots++ : -1;
     const int slot_t = dpost_b || (dgate && post_b) ? slots++ : -1;
-    const BwdArgs a = {dx_out, dh, x_out, y, post_w, gate, row_scale, pre_w, post_stats, pre_stats,
-                       dx, dy, static_cast<float*>(ws), slot_w, slot_b, slot_s, slot_t, slots,
-                       s.n_tokens, s.n_tokens / s.n_groups, s.n_groups, s.d_model, s.pre_norm,
-                       s.post_norm, b.blocks_per_group, b.rows_per_block, s.residual_scale,
-                       s.branch_scale};
-    if (b.blocks > 0) {
-        const unsigned grid = static_cast<unsigned>(b.blocks);
-        by_width(s.d_model, [&](auto team) {
-            using T = decltype(team);
-            constexpr int L = T::kL, W = T::kW, V = T::kV, B = T::kBlock;
-            const bool h32 = s.dh_dtype == VMOE_F32;
+    BwdArgs a = {dx_out, dh, x_out, y, post_w, gate, row_scale, pre_w, post_stats, pre_stats,
+                 dx, dy, static_cast<float*>(ws), slot_w, slot_b, slot_s, slot_t, slots,
+                 s.n_tokens, s.n_tokens / s.n_groups, s.n_groups, s.d_model, s.pre_norm,
+                 s.post_norm, b.blocks_per_group, b.rows_per_block, s.residual_scale,
+                 s.branch_scale, 0};
+    by_width(s.d_model, [&](auto team) {
+        using T = decltype(team);
+        constexpr int L = T::kL, W = T::kW, V = T::kV, B = T::kBlock;
+        const bool h32 = s.dh_dtype == VMOE_F32;
+        for (long long at = 0; at < b.blocks; at += kMostThreads / B) {
+            const unsigned grid = at_most(b.blocks - at, kMostThreads / B);
+            a.first_block = static_cast<int>(at);
             by_flag(s.post_norm != VMOE_NORM_NONE, [&](auto post) {
                 constexpr bool P = decltype(post)::value;
                 using B16 = uint16_t;
@@ -756,8 +764,8 @@ vmoe_status block_norm_bwd_launch(const vmoe_norm_shape& s, const void* dx_out, 
                 else
                     block_norm_bwd_kernel<B16, B16, B16, L, W, V, P><<<grid, B, 0, st>>>(a);
             });
-        });
-    }
+        }
+    });
     if (slots > 0) {
         const int tiles = static_cast<int>(cdiv(s.d_model, kReduceCols));
         const bool merged = dgate && s.n_groups == 1;
@@ -765,15 +773,19 @@ vmoe_status block_norm_bwd_launch(const vmoe_norm_shape& s, const void* dx_out, 
                          (merged ? 0 : (dpost_w != nullptr) + (dpost_b != nullptr));
         const int slices = s.n_groups == 1 ? kSlices : group_slices(b.blocks_per_group);
         const int gates = dgate ? static_cast<int>(cdiv(s.n_groups, kSlices / slices)) : 0;
-        const ReduceArgs r = {static_cast<float*>(ws), post_w, post_b, gate, dpre_w, dpre_b,
-                              dpost_w, dpost_b, dgate, slot_w, slot_b, slot_s, slot_t, slots,
-                              s.n_groups, s.d_model, b.blocks_per_group,
-                              static_cast<int>(b.blocks), tiles, jobs, slices, merged};
-        const unsigned grid = static_cast<unsigned>(tiles) * static_cast<unsigned>(jobs + gates);
-        if (s.dtype == VMOE_F32)
-            block_norm_reduce_kernel<float><<<grid, kReduceCols * kSlices, 0, st>>>(r);
-        else
-            block_norm_reduce_kernel<uint16_t><<<grid, kReduceCols * kSlices, 0, st>>>(r);
+        ReduceArgs r = {static_cast<float*>(ws), post_w, post_b, gate, dpre_w, dpre_b,
+                        dpost_w, dpost_b, dgate, slot_w, slot_b, slot_s, slot_t, slots,
+                        s.n_groups, s.d_model, b.blocks_per_group,
+                        static_cast<int>(b.blocks), tiles, jobs, slices, merged, 0};
+        constexpr int B = kReduceCols * kSlices;
+        const int most = static_cast<int>(kMostThreads / B) / tiles, all = jobs + gates;
+        for (; r.first_job < all; r.first_job += most) {
+            const unsigned grid = at_most(all - r.first_job, most) * tiles;
+            if (s.dtype == VMOE_F32)
+                block_norm_reduce_kernel<float><<<grid, B, 0, st>>>(r);
+            else
+                block_norm_reduce_kernel<uint16_t><<<grid, B, 0, st>>>(r);
+        }
     }
     return launch_status();
 }

@@ -113,3 +113,36 @@ def test_long_groups_of_the_loss(launches, n, g, e, k):
     status, noted = launches(LOSS.format(n=n, g=g, e=e, k=k))
     assert status == V.VMOE_OK
     fits(noted)
+
+
+BACKWARD = """
+    s = Norm({n}, {g}, {d}, 1, 1, 0, 2, 2, 1e-6, 1, 1, 0)
+    lib.vmoe_block_norm_bwd_workspace_bytes.restype = ctypes.c_size_t
+    need = lib.vmoe_block_norm_bwd_workspace_bytes(ctypes.byref(s))
+    status = lib.vmoe_block_norm_bwd(ctypes.byref(s), *[FAKE] * 18, FAKE, ctypes.c_size_t(need), None)
+"""
+
+
+@pytest.mark.parametrize("n, g, d", [
+    (1 << 23, 1 << 23, 8), (1 << 24, 1 << 24, 8), ((1 << 24) + 3, (1 << 24) + 3, 64),
+    (1 << 24, 1 << 24, 256), (1 << 25, 1 << 24, 512), (1 << 22, 1 << 22, 1024),
+    (1 << 28, 1 << 28, 8), (1 << 30, 1, 8), (1 << 30, 1 << 20, 32), (1 << 20, 1, 16384)])
+def test_groups_of_the_norms_backward(launches, n, g, d):
+    status, noted = launches(BACKWARD.format(n=n, g=g, d=d))
+    assert status == V.VMOE_OK
+    fits(noted)
+    rows = [b for b, t in noted if t != 1024 or d > 8192]  # the others add partial rows
+    assert sum(rows) >= max(g, 256)
+
+
+FORWARD = """
+    s = Norm({n}, {g}, {d}, 1, 1, 0, 2, 2, 1e-6, 1, 1, 0)
+    status = lib.vmoe_block_norm_fwd(ctypes.byref(s), *[FAKE] * 12, None)
+"""
+
+
+@pytest.mark.parametrize("n, g, d", [(1 << 30, 1 << 30, 8), (1 << 30, 1, 8), (1 << 24, 2, 16384)])
+def test_rows_of_the_norms_forward(launches, n, g, d):
+    status, noted = launches(FORWARD.format(n=n, g=g, d=d))
+    assert status == V.VMOE_OK
+    fits(noted)
