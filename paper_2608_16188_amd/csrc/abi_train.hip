@@ -40,7 +40,7 @@ namespace {
 
 constexpr int kMaxNormWidth = 16384;
 constexpr long long kMaxChunks = 0x7FFFFFFFLL;
-constexpr long long kMaxValues = 1LL << 36;  // a launch has fewer than 2^32 threads
+constexpr long long kMaxValues = 1LL << 36;
 
 bool known_dtype(int t) { return t == VMOE_F32 || t == VMOE_BF16; }
 bool known_norm(int k) { return k >= VMOE_NORM_NONE && k <= VMOE_NORM_LAYER; }

@@ -531,19 +531,24 @@ vmoe_status adamw_launch(const void* plan, long long n_chunks, const vmoe_adamw_
 vmoe_status state_values_launch(const uint8_t* codes, const uint8_t* scale, bool is_signed,
                                 long long n, void* out, int out_dtype, hipStream_t st) {
     if (n == 0) return VMOE_OK;
-    const unsigned grid = cdiv(n, kValues);
-    if (out_dtype == VMOE_BF16) {
-        uint16_t* o = static_cast<uint16_t*>(out);
-        if (is_signed)
-            state_values_kernel<uint16_t, true><<<grid, kThreads, 0, st>>>(codes, scale, n, o);
-        else
-            state_values_kernel<uint16_t, false><<<grid, kThreads, 0, st>>>(codes, scale, n, o);
-    } else {
-        float* o = static_cast<float*>(out);
-        if (is_signed)
-            state_values_kernel<float, true><<<grid, kThreads, 0, st>>>(codes, scale, n, o);
-        else
-            state_values_kernel<float, false><<<grid, kThreads, 0, st>>>(codes, scale, n, o);
+    constexpr long long kMost = kValues * (1LL << 20);  // a launch has fewer than 2^32 threads
+    for (long long at = 0; at < n; at += kMost) {
+        const long long left = n - at < kMost ? n - at : kMost;
+        const unsigned grid = cdiv(left, kValues);
+        const uint8_t *c = codes + at, *s = scale + at / kStateBlock;
+        if (out_dtype == VMOE_BF16) {
+            uint16_t* o = static_cast<uint16_t*>(out) + at;
+            if (is_signed)
+                state_values_kernel<uint16_t, true><<<grid, kThreads, 0, st>>>(c, s, left, o);
+            else
+                state_values_kernel<uint16_t, false><<<grid, kThreads, 0, st>>>(c, s, left, o);
+        } else {
+            float* o = static_cast<float*>(out) + at;
+            if (is_signed)
+                state_values_kernel<float, true><<<grid, kThreads, 0, st>>>(c, s, left, o);
+            else
+                state_values_kernel<float, false><<<grid, kThreads, 0, st>>>(c, s, left, o);
+        }
     }
     return launch_status();
 }

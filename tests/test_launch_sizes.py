@@ -146,3 +146,33 @@ def test_rows_of_the_norms_forward(launches, n, g, d):
     status, noted = launches(FORWARD.format(n=n, g=g, d=d))
     assert status == V.VMOE_OK
     fits(noted)
+
+
+VALUES = """
+    status = lib.vmoe_adamw_state_values(FAKE, FAKE, 1, L({n}), FAKE, {dtype}, None)
+"""
+
+
+@pytest.mark.parametrize("dtype", [V.VMOE_F32, V.VMOE_BF16])
+@pytest.mark.parametrize("n", [1, 4096, (1 << 36) - 4096, (1 << 36) - 4095, (1 << 36) - 1])
+def test_values_of_states(launches, n, dtype):
+    status, noted = launches(VALUES.format(n=n, dtype=dtype))
+    assert status == V.VMOE_OK
+    fits(noted)
+    assert sum(b for b, _ in noted) == -(-n // 4096)
+
+
+@pytest.mark.parametrize("chunks", [1, 1 << 20, (1 << 20) + 1, (1 << 28) - 1])
+def test_chunks_of_adamw(launches, chunks):
+    text = """
+        class Hyper(ctypes.Structure):
+            _fields_ = [(k, D) for k in "lr b1 b2 eps scale".split()] + \\
+                [("step", L), ("seed", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+        h = Hyper(1e-3, 0.9, 0.99, 1e-8, 1, 1, 0, 0)
+        status = lib.vmoe_adamw(FAKE, L({n}), ctypes.byref(h), None, None) or \\
+            lib.vmoe_grad_norm(FAKE, L({n}), D(1), D(1), FAKE, FAKE, MOST, None)
+    """.format(n=chunks)
+    status, noted = launches(text)
+    assert status == V.VMOE_OK
+    fits(noted)
+    assert sum(b for b, t in noted if t == 128) == 16 * chunks
