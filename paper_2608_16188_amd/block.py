@@ -39,11 +39,16 @@ class SparseBlock:
                  post_norm: str = "none", gate_init: float = 0.1, row_scale: bool = False,
                  w_balance: float = 0.01, w_z: float = 0.001, state_bits: int = 32,
                  weight_decay: float = 0.05, max_norm: float = 1.0, device="cuda"):
-        """norm: of the layer's input and of x_out; post_norm: of the layer's
-        output. row_scale: whether tokens have a scale for the layer's output
-        (drop-path; `self.row_scale`, ones at first). state_bits: 8 keeps AdamW's
-        moments of tensors of 16384 elements or more in 8 bits. The tokens in
-        `inputs` are the stream's first content."""
+        """norm: rms or layer, of the layer's input and of x_out; post_norm: none,
+        rms or layer, of the layer's output. row_scale: whether tokens have a scale
+        for the layer's output (drop-path; `self.row_scale`, ones at first).
+        state_bits: 32, or 8 to keep AdamW's moments of tensors of 16384 elements or
+        more in 8 bits. The tokens in `inputs` are the stream's first content."""
+        for name, value, allowed in (("norm", norm, ("rms", "layer")),
+                                     ("post_norm", post_norm, ("none", "rms", "layer")),
+                                     ("state_bits", state_bits, (8, 32))):
+            if value not in allowed:
+                raise ValueError(f"{name}: one of {allowed} is wanted, got {value!r}")
         self.layer = L = LayerBuffers(cfg, inputs, device)
         self.w_balance, self.w_z, self.max_norm = w_balance, w_z, max_norm
         N, G, d, E = max(cfg.n_tokens, 1), cfg.n_groups, cfg.d_model, cfg.n_experts
