@@ -220,7 +220,12 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
         h.eps = real(a[5]);
         h.grad_scale = real(a[6]);
         h.step = whole(a[7]);
-        h.seed = static_cast<uint32_t>(whole(a[8]));
+        const long long seed = whole(a[8]);
+        if (seed < 0 || seed > 0xFFFFFFFFLL) {
+            PyErr_Format(PyExc_ValueError, "seed: a number of 32 bits is wanted, got %lld", seed);
+            throw Refused();
+        }
+        h.seed = static_cast<uint32_t>(seed);
         void* const clip = pointer(a[9], "clip", kF32, 2);
         return vmoe_adamw(address(a[0]), whole(a[1]), &h, f32(clip), stream_of(a[10]));
     });

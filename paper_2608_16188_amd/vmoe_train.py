@@ -112,7 +112,10 @@ class AdamWTensor:
 
 class AdamWPlan:
     """The chunks of a set of tensors, on the GPU. It keeps the tensors alive;
-    make a new one when a tensor is replaced."""
+    make a new one when a tensor is replaced or its rates change. The random
+    numbers of 8-bit states start at the first tensor's index0 (0 where it gives
+    none): two plans that take the same steps with one seed need an index0 of their
+    own, or seeds of their own, to round with different ones."""
 
     def __init__(self, tensors, device="cuda"):
         self.tensors = list(tensors)
@@ -136,7 +139,9 @@ def vmoe_grad_norm(plan, max_norm, clip, workspace, grad_scale=1.0, stream=None)
 
 def vmoe_adamw(plan, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, clip=None,
                grad_scale=1.0, stream=None):
-    """One step of every tensor of the plan; clip: vmoe_grad_norm's output or None."""
+    """One step of every tensor of the plan; clip: vmoe_grad_norm's output or None.
+    seed: 32 bits, of 8-bit states' random numbers. step, lr and seed are those of
+    this call wherever it is captured and replayed."""
     _check("vmoe_adamw", _train.adamw(plan._address, plan.n_chunks, lr, beta1, beta2, eps,
                                       grad_scale, step, seed, clip, stream))
 
