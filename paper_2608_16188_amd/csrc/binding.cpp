@@ -5,7 +5,7 @@
 // Every function takes its C call's arguments in order (tensors or None; a shape
 // as the ctypes structure; the stream as None, a handle or an object with
 // .cuda_stream) and returns the status. A tensor of the wrong type, layout,
-// device or size raises ValueError before anything is called.
+// device (a launch's are on the current GPU, a plan's on one) or size raises ValueError before anything is called.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <c10/hip/HIPStream.h>
@@ -35,6 +35,19 @@ const at::Tensor& tensor_of(PyObject* o, const char* name) {
     return THPVariable_Unpack(o);
 }
 
+// The GPU that a call's tensors are on: that of the first of them.
+constexpr int kNone = -1;
+thread_local int gpu_of_call = kNone;
+
+void check_gpu(const at::Tensor& t, const char* name) {
+    const int gpu = t.device().index();
+    if (gpu_of_call == kNone) gpu_of_call = gpu;
+    if (gpu == gpu_of_call) return;
+    PyErr_Format(PyExc_ValueError, "%s: a tensor on cuda:%d is wanted, as those before it, got one "
+                 "on cuda:%d", name, gpu_of_call, gpu);
+    throw Refused();
+}
+
 // Pointer of a contiguous tensor of `type` on the GPU with at least `numel`
 // elements; NULL for None.
 void* pointer(PyObject* o, const char* name, at::ScalarType type, int64_t numel) {
@@ -49,6 +62,7 @@ void* pointer(PyObject* o, const char* name, at::ScalarType type, int64_t numel)
                      t.is_contiguous() ? "" : ", not contiguous", t.is_cuda() ? "" : ", not on the GPU");
         throw Refused();
     }
+    check_gpu(t, name);
     return t.data_ptr();
 }
 
@@ -64,13 +78,25 @@ struct Workspace {
             PyErr_SetString(PyExc_ValueError, "workspace: a contiguous tensor on the GPU is wanted");
             throw Refused();
         }
+        check_gpu(t, "workspace");
         p = t.data_ptr();
         bytes = t.nbytes();
     }
 };
 
+// The call's stream, which comes after its tensors: they have to be on the current
+// GPU, as the launch will be.
 void* stream_of(PyObject* o) {
-    if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
+    const bool current = o == Py_None;
+    if (gpu_of_call != kNone || current) {
+        const c10::hip::HIPStream s = c10::hip::getCurrentHIPStream();
+        if (gpu_of_call != kNone && gpu_of_call != s.device_index()) {
+            PyErr_Format(PyExc_ValueError, "tensors on cuda:%d, while the current GPU is cuda:%d",
+                         gpu_of_call, static_cast<int>(s.device_index()));
+            throw Refused();
+        }
+        if (current) return s.stream();
+    }
     PyObject* handle = PyObject_GetAttrString(o, "cuda_stream");
     if (handle == nullptr) {
         PyErr_Clear();
@@ -118,11 +144,7 @@ long long whole(PyObject* o) {
     if (v == -1 && PyErr_Occurred()) throw Refused();
     return v;
 }
-void* address(PyObject* o) {
-    void* p = PyLong_AsVoidPtr(o);
-    if (p == nullptr && PyErr_Occurred()) throw Refused();
-    return p;
-}
+void* plan_of(PyObject* o) { return pointer(o, "plan", kU8, 0); }
 
 // Argument count, C++ exceptions to Python ones, status to int.
 template <typename F>
@@ -131,6 +153,7 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t wanted, F f) {
         PyErr_Format(PyExc_TypeError, "%zd arguments are wanted, got %zd", wanted, got);
         return nullptr;
     }
+    gpu_of_call = kNone;
     try {
         return PyLong_FromLong(f());
     } catch (const Refused&) {
@@ -200,17 +223,17 @@ PyObject* load_balance_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// (plan address, chunks, grad_scale, max_norm, clip, workspace, stream)
+// (plan or None, chunks, grad_scale, max_norm, clip, workspace, stream)
 PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 7, [&] {
         const Workspace ws(a[5]);
-        void* const clip = pointer(a[4], "clip", kF32, 2);
-        return vmoe_grad_norm(address(a[0]), whole(a[1]), real(a[2]), real(a[3]), f32(clip), ws.p,
+        void *const plan = plan_of(a[0]), *const clip = pointer(a[4], "clip", kF32, 2);
+        return vmoe_grad_norm(plan, whole(a[1]), real(a[2]), real(a[3]), f32(clip), ws.p,
                               ws.bytes, stream_of(a[6]));
     });
 }
 
-// (plan address, chunks, lr, beta1, beta2, eps, grad_scale, step, seed, clip, stream)
+// (plan or None, chunks, lr, beta1, beta2, eps, grad_scale, step, seed, clip, stream)
 PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 11, [&] {
         vmoe_adamw_hyper h = {};
@@ -226,8 +249,8 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
             throw Refused();
         }
         h.seed = static_cast<uint32_t>(seed);
-        void* const clip = pointer(a[9], "clip", kF32, 2);
-        return vmoe_adamw(address(a[0]), whole(a[1]), &h, f32(clip), stream_of(a[10]));
+        void *const plan = plan_of(a[0]), *const clip = pointer(a[9], "clip", kF32, 2);
+        return vmoe_adamw(plan, whole(a[1]), &h, f32(clip), stream_of(a[10]));
     });
 }
 
@@ -303,6 +326,7 @@ vmoe_adamw_tensor tensor_entry(PyObject* o, uint64_t& next) {
 
 // (list of AdamWTensor) -> (status, chunks, plan as bytes)
 PyObject* adamw_plan(PyObject*, PyObject* list) {
+    gpu_of_call = kNone;
     try {
         const Held items(PySequence_Fast(list, "tensors: a sequence is wanted"));
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(items.o);

@@ -4,9 +4,9 @@ Block norm, load-balance loss and AdamW of a sparse block's training step.
 Functions have the names and argument order of the C calls and take torch
 device tensors (or None for optional pointers); all arithmetic runs in
 libvmoe.so. Marshalling runs in the extension module _train, which also checks
-what a pointer cannot say: a tensor's type, that it is contiguous, on the GPU
-and large enough (ValueError); everything else is the library's status
-(VmoeError). A missing library or extension raises at import.
+what a pointer cannot say: a tensor's type, that it is contiguous, on the
+current GPU as the others are and large enough (ValueError); everything else is
+the library's status (VmoeError). A missing library or extension raises at import.
 """
 from __future__ import annotations
 
@@ -124,7 +124,10 @@ class AdamWPlan:
         host = torch.frombuffer(bytearray(table), dtype=torch.uint8) if table else \
             torch.zeros(1, dtype=torch.uint8)
         self.table = host.to(device)
-        self._address = self.table.data_ptr()
+        if self.tensors and self.table.device != self.tensors[0].param.device:
+            raise ValueError(f"device: the tensors are on {self.tensors[0].param.device}, the plan "
+                             f"would be on {self.table.device}")
+        self._entries = self.table if self.n_chunks else None
 
 
 def vmoe_grad_norm_workspace_bytes(plan: AdamWPlan) -> int:
@@ -133,7 +136,7 @@ def vmoe_grad_norm_workspace_bytes(plan: AdamWPlan) -> int:
 
 def vmoe_grad_norm(plan, max_norm, clip, workspace, grad_scale=1.0, stream=None):
     """clip [2] f32 out: norm of all gradients, factor for vmoe_adamw."""
-    _check("vmoe_grad_norm", _train.grad_norm(plan._address, plan.n_chunks, grad_scale, max_norm,
+    _check("vmoe_grad_norm", _train.grad_norm(plan._entries, plan.n_chunks, grad_scale, max_norm,
                                               clip, workspace, stream))
 
 
@@ -142,7 +145,7 @@ def vmoe_adamw(plan, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, clip=
     """One step of every tensor of the plan; clip: vmoe_grad_norm's output or None.
     seed: 32 bits, of 8-bit states' random numbers. step, lr and seed are those of
     this call wherever it is captured and replayed."""
-    _check("vmoe_adamw", _train.adamw(plan._address, plan.n_chunks, lr, beta1, beta2, eps,
+    _check("vmoe_adamw", _train.adamw(plan._entries, plan.n_chunks, lr, beta1, beta2, eps,
                                       grad_scale, step, seed, clip, stream))
 
 
