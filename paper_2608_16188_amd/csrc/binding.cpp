@@ -352,6 +352,8 @@ PyObject* adamw_plan(PyObject*, PyObject* list) {
 // (codes, scale, is_signed, out, stream)
 PyObject* adamw_state_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 5, [&] {
+        const int is_signed = PyObject_IsTrue(a[2]);
+        if (is_signed < 0) throw Refused();
         const int64_t count = tensor_of(a[0], "codes").numel();
         const at::Tensor& out = tensor_of(a[3], "out");
         const int32_t dtype = float_type(out, "out");
@@ -359,7 +361,7 @@ PyObject* adamw_state_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
                            pointer(a[1], "scale", kU8, (count + 127) / 128),
                            pointer(a[3], "out", out.scalar_type(), count)};
         return vmoe_adamw_state_values(static_cast<uint8_t*>(p[0]), static_cast<uint8_t*>(p[1]),
-                                       PyObject_IsTrue(a[2]), count, p[2], dtype, stream_of(a[4]));
+                                       is_signed, count, p[2], dtype, stream_of(a[4]));
     });
 }
 

@@ -1,5 +1,6 @@
 """What the binding of vmoe_train.h refuses in arguments that are no tensors (no GPU)."""
 import pytest
+import torch
 
 from paper_2608_16188_amd import vmoe_train as T
 
@@ -36,3 +37,13 @@ def test_a_plan_away_from_its_tensors_refused():
     a = Elsewhere(1, 0)
     with pytest.raises(ValueError, match="^device: .*cuda:1.*cpu"):
         T.AdamWPlan([T.AdamWTensor(a, a, a, a)], device="cpu")
+
+
+def test_a_flag_that_has_no_truth_value_says_so():
+    class Odd:
+        def __bool__(self):
+            raise KeyError("no truth value")
+
+    z = torch.zeros(128, dtype=torch.uint8)
+    with pytest.raises(KeyError, match="no truth value"):
+        T.vmoe_adamw_state_values(z, z, Odd(), torch.zeros(128))
