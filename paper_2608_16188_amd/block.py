@@ -27,11 +27,14 @@ NORMS = {"none": T.VMOE_NORM_NONE, "rms": T.VMOE_NORM_RMS, "layer": T.VMOE_NORM_
 
 
 def _current(stream):
-    """Context in which `stream` (None, a torch stream or a handle) is the current one."""
+    """Context in which `stream` is the current one: None, a handle, or anything
+    with .cuda_stream, as the calls take it."""
     if stream is None:
         return contextlib.nullcontext()
-    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream")
-                             else torch.cuda.ExternalStream(stream))
+    handle = getattr(stream, "cuda_stream", stream)
+    # an ExternalStream of handle 0 would be a new stream
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle) if handle
+                             else torch.cuda.default_stream())
 
 
 class SparseBlock:

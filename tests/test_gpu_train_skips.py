@@ -60,6 +60,32 @@ def test_skipped_steps_do_not_count(pattern, bits):
             assert same_bits(a.states[k][s], b.states[k][s]), (k, s)
 
 
+class Holder:
+    def __init__(self, stream):
+        self.cuda_stream = stream.cuda_stream
+
+
+@pytest.mark.parametrize("kind", ["stream", "handle", "holder", "default handle"])
+def test_streams_as_the_calls_take_them(kind):
+    """On a stream that waits: what runs on another one would meet old gradients."""
+    a, b = make(32), make(32)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    ups = [torch.randn(96, 64, device="cuda", generator=gen) for _ in range(3)]
+    for up in ups:
+        go(a, up)
+    torch.cuda.synchronize()
+    side = torch.cuda.default_stream() if kind == "default handle" else torch.cuda.Stream()
+    given = {"stream": side, "handle": side.cuda_stream, "holder": Holder(side),
+             "default handle": 0}[kind]
+    for up in ups:
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2_000_000)
+        go(b, up, given)
+    side.synchronize()
+    assert a.steps == b.steps == 3
+    assert all(same_bits(a.params[k], p) for k, p in b.params.items())
+
+
 def test_steps_can_be_set():
     """As when training goes on from saved parameters and states."""
     a, b = make(32), make(32)
