@@ -6,9 +6,11 @@
 // norms need: means and deviations are sums over the team (lane moves within a
 // wave, LDS across waves). Both directions are streams of rows, bound by HBM:
 // 36928 rows of 1024 in bf16 take 53 us forward (297 MB, 5.6 TB/s) and 105 us
-// backward (529 MB, 5.1 TB/s), and a copy of 256 MiB runs at 5.4 TB/s. The rows'
-// stores stay in the caches for the call that reads them next: stores past them
-// make the backward alone 2 to 20 % faster, and it with its reader 3 to 5 % slower.
+// backward (529 MB, 5.1 TB/s); all in f32 119 us and, with the column sums'
+// launch, 187 (605 and 908 MB). A copy of 256 MiB runs at 5.4 TB/s, AdamW's update
+// at 6.4. The rows' stores stay in the caches for the call that reads them next:
+// stores past them make the backward alone 2 to 20 % faster, and it with its
+// reader 3 to 5 % slower.
 //
 // The backward also sums over tokens for each column (the gradients of weights,
 // biases and gate). A team keeps those sums in registers over all of its rows;
@@ -670,7 +672,9 @@ struct BwdGrid {
 
 // As many blocks as are resident (two of four waves on a CU, one of more), no
 // block across two groups, a row or more for every wave of one. More blocks
-// would only leave more partial rows.
+// would only leave more partial rows. Groups of a few rows take a block each all the
+// same, with idle waves and four partial rows a group (36864 x 1024: 111 us with 1024
+// groups, 170 with 9216; 36928 with a group a row 523).
 BwdGrid bwd_grid(const vmoe_norm_shape& s) {
     const int Ng = s.n_tokens / s.n_groups;
     if (Ng == 0) return {1, 1, 0};
