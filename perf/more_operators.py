@@ -149,18 +149,18 @@ def prepare(case, seed):
 
 def _handles(s):
     """The shape, buffers and outputs that a program makes once."""
-    from paper_2608_16188_amd import vmoe_train as T
+    from paper_2608_16188_amd import vmoe_head as H
     c, n, d, V = s["case"], s["case"]["rows"], s["case"]["d"], s["case"]["classes"]
-    dt = T.VMOE_BF16 if c["dtype"] == "bf16" else T.VMOE_F32
-    s["shape"] = sh = T.make_head_shape(n, d, V, dt, n_teacher=c["top"],
+    dt = H.VMOE_BF16 if c["dtype"] == "bf16" else H.VMOE_F32
+    s["shape"] = sh = H.make_head_shape(n, d, V, dt, n_teacher=c["top"],
                                         temperature=c["temperature"])
     new = lambda dtype, *shape: torch.empty(*shape, dtype=dtype, device=DEV)  # noqa: E731
     bytes_ = lambda k: new(torch.uint8, max(k, 16))  # noqa: E731
-    s["saved"] = bytes_(T.vmoe_head_loss_saved_bytes(sh))
-    s["fwd_ws"] = bytes_(T.vmoe_head_loss_fwd_workspace_bytes(sh))
+    s["saved"] = bytes_(H.vmoe_head_loss_saved_bytes(sh))
+    s["fwd_ws"] = bytes_(H.vmoe_head_loss_fwd_workspace_bytes(sh))
     s["out"] = dict(losses=new(torch.float32, 4), row_losses=new(torch.float32, n, 2))
     if c["pass"] != "eval":
-        s["bwd_ws"] = bytes_(T.vmoe_head_loss_bwd_workspace_bytes(sh))
+        s["bwd_ws"] = bytes_(H.vmoe_head_loss_bwd_workspace_bytes(sh))
         s["out"]["dx"] = new(_t(c["dtype"]), n, d)
         if c["pass"] == "train":
             s["out"]["dweight"] = new(_t(c["dtype"]), V, d)
@@ -169,13 +169,13 @@ def _handles(s):
 
 
 def _run_own(s):
-    from paper_2608_16188_amd import vmoe_train as T
+    from paper_2608_16188_amd import vmoe_head as H
     o = s["out"]
-    T.vmoe_head_loss_fwd(s["shape"], s["x"], s["weight"], s["bias"], s["labels"], s["teacher_idx"],
+    H.vmoe_head_loss_fwd(s["shape"], s["x"], s["weight"], s["bias"], s["labels"], s["teacher_idx"],
                          s["teacher_logits"], s["row_weight"], o["losses"], o["row_losses"],
                          s["saved"], s["fwd_ws"])
     if s["case"]["pass"] != "eval":
-        T.vmoe_head_loss_bwd(s["shape"], s["weight"], s["bias"], s["saved"], s["w_label"],
+        H.vmoe_head_loss_bwd(s["shape"], s["weight"], s["bias"], s["saved"], s["w_label"],
                              s["w_teacher"], o["dx"], o.get("dweight"), o.get("dbias"),
                              s["bwd_ws"])
     return dict(o)
