@@ -175,7 +175,7 @@ def _run_own(s):
                          s["teacher_logits"], s["row_weight"], o["losses"], o["row_losses"],
                          s["saved"], s["fwd_ws"])
     if s["case"]["pass"] != "eval":
-        H.vmoe_head_loss_bwd(s["shape"], s["weight"], s["bias"], s["saved"], s["w_label"],
+        H.vmoe_head_loss_bwd(s["shape"], s["weight"], s["saved"], s["w_label"],
                              s["w_teacher"], o["dx"], o.get("dweight"), o.get("dbias"),
                              s["bwd_ws"])
     return dict(o)
