@@ -1,0 +1,96 @@
+/*
+ * vmoe_head.h -- what a training step learns from: a head over many classes
+ * with its losses, softmax cross entropy against labels and distillation from a
+ * teacher's top logits. Entry points of libvmoe.so.
+ *
+ * The conventions of vmoe.h and vmoe_train.h hold: device pointers owned by the
+ * caller, 16-byte aligned, row-major and contiguous; work enqueued on `stream`
+ * without synchronising; no allocation; status codes, checked before anything is
+ * enqueued; required pointers checked whatever the sizes. A workspace needs no
+ * clearing and holds nothing between calls. Every sum is taken in a fixed order
+ * (no float atomics): the same inputs give the same bits.
+ */
+#ifndef VMOE_HEAD_H
+#define VMOE_HEAD_H
+
+#include "vmoe_train.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum { VMOE_REDUCE_MEAN = 0, VMOE_REDUCE_SUM = 1 } vmoe_reduction;
+
+/* Most entries of a teacher's list. */
+#define VMOE_HEAD_MAX_TEACHER 256
+
+typedef struct vmoe_head_shape {
+    int32_t n_rows;      /* N >= 0, at most 2^21 (else UNSUPPORTED)                   */
+    int32_t d_model;     /* d, multiple of 8, at most 65536; N d < 2^30 (else UNSUPPORTED) */
+    int32_t n_classes;   /* V >= 1, at most 2^24; N V < 2^36 (else UNSUPPORTED)       */
+    int32_t n_teacher;   /* K in [0, 256]: entries of the teacher's list; 0: none     */
+    int32_t dtype;       /* x, weight, bias and every gradient (vmoe_dtype)           */
+    int32_t reduction;   /* vmoe_reduction                                            */
+    float temperature;   /* T of the distillation, in [2^-10, 2^10]                   */
+    int32_t reserved;    /* must be 0                                                 */
+} vmoe_head_shape;
+
+/* Bytes of `saved` and of the calls' scratch (0 on an invalid shape). Neither
+ * grows with N V: the logits are formed a tile at a time and never stored, their
+ * gradient a piece of the classes at a time, within 1 GiB of the workspace. */
+size_t vmoe_head_loss_saved_bytes(const vmoe_head_shape* shape);
+size_t vmoe_head_loss_fwd_workspace_bytes(const vmoe_head_shape* shape);
+size_t vmoe_head_loss_bwd_workspace_bytes(const vmoe_head_shape* shape);
+
+/* The losses of a head over rows of x, z = x weight^T + bias [N, V] (not stored):
+ *   label loss of row t, where labels[t] lies in [0, V):
+ *     a_t = lse(z_t) - z_t[labels[t]],  lse(z) = log sum_c exp z[c]
+ *   teacher loss of row t, over the entries j whose teacher_idx[t,j] = c_j lies in
+ *   [0, V) and whose logit is not -infinity, where there is one:
+ *     q_j = softmax of teacher_logits[t,j] / T over those entries
+ *     b_t = T^2 sum_j q_j (log q_j - log softmax(z_t / T)[c_j])
+ *     (a class listed twice counts as two entries)
+ *   losses[0] = sum_t w_t a_t / losses[2], losses[2] = sum of w_t over rows with a label
+ *   losses[1] = sum_t w_t b_t / losses[3], losses[3] = sum of w_t over rows with a teacher
+ * with w_t = row_weight[t], or 1. REDUCE_SUM leaves out the division. A mean over
+ * weights whose sum is 0 is 0.
+ *   x [N, d], weight [V, d], bias [V] or NULL                          dtype
+ *   labels [N] i32 or NULL: any value outside [0, V) is no label
+ *   teacher_idx [N, K] i32, teacher_logits [N, K] f32: NULL exactly if K is 0
+ *   row_weight [N] f32 or NULL
+ *   losses [4] f32 out; row_losses [N, 2] f32 out or NULL: a_t, b_t (0 without)
+ *   saved: vmoe_head_loss_saved_bytes(shape) bytes out, for the backward
+ * labels or a teacher has to be given. Rows with neither, or whose weight is 0, are
+ * left out: their rows of x, and their teacher_logits, are not read and may hold
+ * anything, and so may the logits of entries without a class. Such rows cost nothing
+ * in the products. bf16 products run on matrix cores with f32 accumulation, f32
+ * ones in f32; lse, q and losses are f32, sums over rows double. */
+vmoe_status vmoe_head_loss_fwd(const vmoe_head_shape* shape, const void* x, const void* weight,
+                               const void* bias, const int32_t* labels,
+                               const int32_t* teacher_idx, const float* teacher_logits,
+                               const float* row_weight, float* losses, float* row_losses,
+                               void* saved, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/* Gradients of w_label losses[0] + w_teacher losses[1] of the forward that wrote
+ * `saved`, at the same weight:
+ *   dz[t] = g_t (softmax(z_t) - 1[labels[t]])
+ *           + h_t (softmax(z_t / T) - sum_j q_j 1[c_j])
+ *   g_t = w_label w_t / losses[2], h_t = w_teacher T w_t / losses[3]
+ *   (0 for a row without label, or without teacher; REDUCE_SUM: no division)
+ *   dx = dz weight [N, d] (0 for rows that were left out),
+ *   dweight = dz^T x [V, d], dbias = sum_t dz [V]               dtype, overwritten
+ * Each of them may be NULL and is not formed then (a frozen head, or a head alone).
+ * The logits are formed again. bf16: dz is rounded to bf16 for the products, as every
+ * operand of theirs is; they and the sums accumulate in f32 and are rounded once.
+ * `saved` is read only: several backwards may follow one forward. */
+vmoe_status vmoe_head_loss_bwd(const vmoe_head_shape* shape, const void* weight,
+                               const void* saved, float w_label, float w_teacher, void* dx,
+                               void* dweight, void* dbias, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* VMOE_HEAD_H */

@@ -19,11 +19,12 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libvmoe.so")
-BINDING = os.path.join(PKG, "_train.so")  # Python's side of vmoe_train.h
+BINDING = os.path.join(PKG, "_train.so")  # Python's side of vmoe_train.h and vmoe_head.h
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["abi.hip", "route.hip", "moves.hip", "ffn.hip", "route_bwd.hip", "balance.hip",
-           "abi_train.hip", "block_norm.hip", "gate_loss.hip", "adamw.hip", "grouping.cpp"]
+           "abi_train.hip", "block_norm.hip", "gate_loss.hip", "adamw.hip", "abi_head.hip",
+           "head_loss.hip", "grouping.cpp"]
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 PER_FILE = {"route.hip": ["-ffp-contract=off"], "grouping.cpp": ["-ffp-contract=off"],

@@ -1,4 +1,4 @@
-// Python calls of vmoe_train.h (module _train). A launch takes a few
+// Python calls of vmoe_train.h and vmoe_head.h (module _train). A launch takes a few
 // microseconds on the host, which small calls wait for: argument checks and
 // marshalling in Python cost 5 to 8 us a call, here less than one.
 //
@@ -15,7 +15,7 @@
 #include <exception>
 #include <vector>
 
-#include "../../include/vmoe_train.h"
+#include "../../include/vmoe_head.h"
 
 namespace {
 
@@ -365,6 +365,51 @@ PyObject* adamw_state_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// What the forward leaves for the backward: u8, at least as much as the shape asks for
+// (0 where the library will refuse the shape).
+void* saved_of(PyObject* o, const vmoe_head_shape* s) {
+    return pointer(o, "saved", kU8, static_cast<int64_t>(vmoe_head_loss_saved_bytes(s)));
+}
+
+// (shape, x, weight, bias, labels, teacher_idx, teacher_logits, row_weight, losses,
+// row_losses, saved, workspace, stream)
+PyObject* head_loss_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&] {
+        const Shape<vmoe_head_shape> s(a[0], "HeadShape");
+        const at::ScalarType act = scalar(s->dtype);
+        const int64_t rows = s->n_rows, d = s->d_model, V = s->n_classes, K = s->n_teacher;
+        void* const p[] = {
+            pointer(a[1], "x", act, rows * d), pointer(a[2], "weight", act, V * d),
+            pointer(a[3], "bias", act, V), pointer(a[4], "labels", kI32, rows),
+            pointer(a[5], "teacher_idx", kI32, rows * K),
+            pointer(a[6], "teacher_logits", kF32, rows * K),
+            pointer(a[7], "row_weight", kF32, rows), pointer(a[8], "losses", kF32, 4),
+            pointer(a[9], "row_losses", kF32, 2 * rows), saved_of(a[10], s.get())};
+        const Workspace ws(a[11]);
+        return vmoe_head_loss_fwd(s.get(), p[0], p[1], p[2], static_cast<int32_t*>(p[3]),
+                                  static_cast<int32_t*>(p[4]), f32(p[5]), f32(p[6]), f32(p[7]),
+                                  f32(p[8]), p[9], ws.p, ws.bytes, stream_of(a[12]));
+    });
+}
+
+// (shape, weight, saved, w_label, w_teacher, dx, dweight, dbias, workspace, stream)
+PyObject* head_loss_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&] {
+        const Shape<vmoe_head_shape> s(a[0], "HeadShape");
+        const at::ScalarType act = scalar(s->dtype);
+        const int64_t rows = s->n_rows, d = s->d_model, V = s->n_classes;
+        void* const p[] = {pointer(a[1], "weight", act, V * d), saved_of(a[2], s.get()),
+                           pointer(a[5], "dx", act, rows * d),
+                           pointer(a[6], "dweight", act, V * d),
+                           pointer(a[7], "dbias", act, V)};
+        const Workspace ws(a[8]);
+        const float w_label = static_cast<float>(real(a[3]));
+        const float w_teacher = static_cast<float>(real(a[4]));
+        return vmoe_head_loss_bwd(s.get(), p[0], p[1], w_label, w_teacher, p[2], p[3], p[4], ws.p,
+                                  ws.bytes, stream_of(a[9]));
+    });
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL,
@@ -374,13 +419,15 @@ PyMethodDef method(const char* name) {
 PyMethodDef methods[] = {method<block_norm_fwd>("block_norm_fwd"),
                          method<block_norm_bwd>("block_norm_bwd"),
                          method<load_balance_loss>("load_balance_loss"),
+                         method<head_loss_fwd>("head_loss_fwd"),
+                         method<head_loss_bwd>("head_loss_bwd"),
                          method<grad_norm>("grad_norm"),
                          method<adamw>("adamw"),
                          {"adamw_plan", adamw_plan, METH_O, nullptr},
                          method<adamw_state_values>("adamw_state_values"),
                          {nullptr, nullptr, 0, nullptr}};
 
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train", "Calls of vmoe_train.h", -1, methods,
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train", "Calls of vmoe_train.h and vmoe_head.h", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,1447 @@
+// A head over many classes with its losses (vmoe_head.h) on gfx950.
+//
+// z = x W^T + b is never stored. The forward forms it a tile at a time and keeps of
+// each row and strip of columns the largest value and the sum of exponentials; the
+// backward forms it again, turns it into dz a piece of the classes at a time and
+// multiplies that piece by W and by x:
+//   mark      which rows have a label or a teacher, their places among those
+//             (1024 rows a block); the bias in f32, -infinity past the classes
+//   rows      a wave a row: the row's x to its place, its label and its teacher's
+//             entries with their q
+//   targets   the logits of those classes, by the same chain of matrix instructions
+//             as the tiles', so that they have the tiles' bits
+//   stats     z by tiles -> (max, sum of exponentials) of each row and strip
+//   finish    lse of each row, its losses, their sums (last block, double)
+// and for each piece of the classes
+//   grad_z    z by tiles -> dz but for the targets, in the operands' type
+//   subtract  dz at the targets, in f32 from their logits, rounded once
+//   product   dx += dz W (f32 partial sums in slots), dW = dz^T x, db = sums of dz
+// and in the end dx from the slots, rounded once, rows back to their places.
+// Only live rows reach the products: their number is read on the device, tiles past
+// it end at once, so padding costs nothing and the host waits for nothing.
+//
+// z twice costs 2 N V d products more than the 6 N V d of keeping it; kept in f32 it
+// would be written, read and written again as dz, 10 bytes a logit: at 5 TB/s and
+// 1 PFLOP/s as long as the products at d = 1024, and memory that grows with N V.
+#include <math.h>
+
+#include "../../include/vmoe_head.h"
+#include "common_train.h"
+#include "gemm_tile.h"
+
+namespace vmoe {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kMarkRows = 1024;
+constexpr int kCus = 256;
+constexpr size_t kPieceBytes = size_t(1) << 30;  // dz of one piece of the classes
+// Stands for the maximum of a strip without a class: its -infinities give sums of 0
+// (with -infinity itself, differences would be NaN).
+constexpr float kLowest = -1e30f;
+
+size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+// ------------------------------------------------------------------ layout
+
+struct Header {
+    int32_t live;      // rows with a label or a teacher
+    int32_t labelled;  // labels were given
+    float sum[2];      // of weights: rows with a label, with a teacher
+};
+
+// What the forward leaves for the backward. Rows are live ones, in their order, but
+// for `place`.
+struct Saved {
+    Header* head;
+    int32_t* row;    // [N] the row's number among all
+    int32_t* place;  // [N] of all rows: their place, -1 where left out
+    float4* rec;     // [N] max z, log2 of the sums of exp(z - max) and of its T-th root,
+                     //     sum_j q_j log q_j
+    float2* weight;  // [N] weights in the two losses
+    float* bias;     // [V up to 256] f32, -infinity from V on
+    int32_t* tidx;   // [N, 1 + K] the label and the entries' classes, -1 without
+    float* tz;       // [N, 1 + K] their logits
+    float* tq;       // [N, 1 + K] 1 and q
+    void* x;         // [N, d]
+    size_t bytes;
+};
+
+int padded_classes(const vmoe_head_shape& s) { return static_cast<int>(up256(s.n_classes)); }
+size_t elem_bytes(const vmoe_head_shape& s) { return s.dtype == VMOE_BF16 ? 2 : 4; }
+
+struct Carver {
+    char* p;
+    size_t off = 0;
+    template <typename T>
+    T* take(size_t n) {
+        T* q = p ? reinterpret_cast<T*>(p + off) : nullptr;
+        off += up256(n * sizeof(T));
+        return q;
+    }
+};
+
+Saved saved_layout(const vmoe_head_shape& s, void* base) {
+    Carver c{static_cast<char*>(base)};
+    const size_t N = s.n_rows, E = N * (1 + s.n_teacher);
+    Saved v;
+    v.head = c.take<Header>(1);
+    v.row = c.take<int32_t>(N);
+    v.place = c.take<int32_t>(N);
+    v.rec = c.take<float4>(N);
+    v.weight = c.take<float2>(N);
+    v.bias = c.take<float>(padded_classes(s));
+    v.tidx = c.take<int32_t>(E);
+    v.tz = c.take<float>(E);
+    v.tq = c.take<float>(E);
+    v.x = c.take<char>(N * s.d_model * elem_bytes(s));
+    v.bytes = c.off;
+    return v;
+}
+
+// ------------------------------------------------------------------ tilings
+
+// f32: 128 x 128 tiles of four waves as 2 x 2, 16-deep stages; a wave's rows and
+// columns lie in the tile as in the phased bf16 tiles (64 wm + 32 i, 64 b + 32 wn).
+struct F32Tile {
+    static constexpr int PB = 2, BM = 128, BN = 128, WGN = 2, NT = 256, FM = 2, WM = 64;
+    static constexpr int KB = 16, OP_EL = BM * KB;
+};
+using TileBig = PhaseTile<4>;
+using TileNarrow = PhaseTile<3>;
+
+template <class T>
+constexpr bool is_f32() { return std::is_same<T, F32Tile>::value; }
+template <class T>
+using Elm = typename std::conditional<is_f32<T>(), float, uint16_t>::type;
+
+// ------------------------------------------------------------------ products
+
+// A product C[m, n] = sum_k A(m, k) B(n, k) cut into tiles, and k into `splits`
+// ranges of whole stages. `live`: the number of rows of x, which bounds m (or k where
+// the rows are summed over).
+struct Product : GemmArgs {
+    const int32_t* live;
+    int rows_are_k;
+    int tiles_n, splits, group_m, chunk;
+};
+
+struct StatsArgs : Product {
+    const float* zbias;  // [V up to 256]
+    float *mx, *sum, *sum_t;  // [strips][N]
+    int n_rows;
+    float scale, scale_t;     // log2 e / temperature of `sum` and of `sum_t`
+    static constexpr int OUT = EPI_STORE;
+};
+
+struct GradZArgs : Product {
+    const float* zbias;
+    const Header* head;
+    const float4* rec;
+    const float2* weight;
+    void* dz;  // [N, ldz]
+    int ldz;
+    float w_label, w_teacher;  // w_teacher times T
+    float inv_t;
+    int mean, teacher;
+    static constexpr int OUT = EPI_STORE;
+};
+
+struct PartArgs : Product {  // f32 sums of each range of k
+    float* part;       // [splits][M, N]
+    size_t part_stride;
+    float* part_sums;  // [splits][M] of A's rows, or null
+    int add;           // to what is there
+    static constexpr int OUT = EPI_F32;
+};
+
+struct StoreArgs : Product {  // rounded, k in one range
+    void* c;      // [M, N], or null
+    void* sums;   // [M] of A's rows, or null
+    static constexpr int OUT = EPI_F32;
+};
+
+// The tile that finish_tile is called for.
+template <class ARGS>
+struct Tiled : ARGS {
+    int t_m0, t_n0, t_n, t_split;  // first row and column, number of the column of tiles
+};
+
+// Block b runs on XCD b mod 8; XCDs take chunks of neighbouring tiles in turn, and
+// tiles go in groups of group_m rows of tiles, so that an XCD's blocks share operand
+// panels in its L2.
+template <int BM, class ARGS>
+__device__ __forceinline__ bool take_tile(const ARGS& p, int M, int* tm, int* tn, int* split) {
+    const int l = blockIdx.x >> 3;
+    int w = ((l / p.chunk) * 8 + (blockIdx.x & 7)) * p.chunk + l % p.chunk;
+    const int tiles_m = (M + BM - 1) / BM, tiles = tiles_m * p.tiles_n;
+    if (w >= tiles * p.splits) return false;
+    *split = w / tiles;
+    w -= *split * tiles;
+    const int grp = w / (p.group_m * p.tiles_n);
+    const int gm = min(p.group_m, tiles_m - grp * p.group_m);
+    const int idx = w - grp * p.group_m * p.tiles_n;
+    *tm = grp * p.group_m + idx % gm;
+    *tn = idx / gm;
+    return true;
+}
+
+__device__ __forceinline__ uint32_t record_bytes(long long bytes) {
+    return static_cast<uint32_t>(bytes < 0x7FFFFFF0LL ? bytes : 0x7FFFFFF0LL);
+}
+
+template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
+__device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const float* b, int M,
+                                         int N, int K, float* lds);
+
+// One tile: the operands are taken from the tile's corner and its range of k on, so that
+// offsets inside it fit 32 bits however large they are.
+template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
+__device__ __forceinline__ bool place_tile(const ARGS& args, Tiled<ARGS>* p, const Elm<T>** a,
+                                           const Elm<T>** b, int* M, int* N, int* K) {
+    const int live = *args.live;
+    const int rows = args.rows_are_k ? args.M : min(live, args.M);
+    const int depth = args.rows_are_k ? min(live, args.K) : args.K;
+    int tm, tn, split;
+    if (!take_tile<T::BM>(args, rows, &tm, &tn, &split)) return false;
+    tm = __builtin_amdgcn_readfirstlane(tm);
+    tn = __builtin_amdgcn_readfirstlane(tn);
+    split = __builtin_amdgcn_readfirstlane(split);
+    static_cast<ARGS&>(*p) = args;
+    p->t_m0 = tm * T::BM;
+    p->t_n0 = tn * T::BN;
+    p->t_n = tn;
+    p->t_split = split;
+    // (ranges of 64 k, the deepest stage)
+    const int runs = (depth + 63) / 64;
+    const int k0 = 64 * static_cast<int>(static_cast<long long>(runs) * split / args.splits);
+    const int k1 = min(depth, 64 * static_cast<int>(static_cast<long long>(runs) * (split + 1) /
+                                                    args.splits));
+    *M = rows - p->t_m0;
+    *N = args.N - p->t_n0;
+    *K = k1 - k0;
+    const size_t m0 = p->t_m0, n0 = p->t_n0, lda = args.a.ld, ldb = args.b.ld;
+    *a = static_cast<const Elm<T>*>(args.a.base) + (A_KMAJOR ? m0 * lda + k0 : k0 * lda + m0);
+    *b = static_cast<const Elm<T>*>(args.b.base) + (B_KMAJOR ? n0 * ldb + k0 : k0 * ldb + n0);
+    return true;
+}
+
+template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
+__global__ __launch_bounds__(T::NT)
+__attribute__((amdgpu_waves_per_eu(2, 2)))
+void product_bf16_kernel(ARGS args) {
+    __shared__ __attribute__((aligned(1024))) uint16_t a0[T::A_EL];
+    __shared__ __attribute__((aligned(1024))) uint16_t a1[T::A_EL];
+    __shared__ __attribute__((aligned(1024))) uint16_t bl0[T::BL_EL];
+    __shared__ __attribute__((aligned(1024))) uint16_t bh0[T::BH_EL];
+    __shared__ __attribute__((aligned(1024))) uint16_t bl1[T::BL_EL];
+    __shared__ __attribute__((aligned(1024))) uint16_t bh1[T::BH_EL];
+    __shared__ __attribute__((aligned(1024))) uint16_t stg[T::S_EL];
+    Tiled<ARGS> p;
+    const uint16_t *a, *b;
+    int M, N, K;
+    if (!place_tile<T, A_KMAJOR, B_KMAJOR>(args, &p, &a, &b, &M, &N, &K)) return;
+    // bytes from the corner on: of a tile's rows, or of a range's k rows
+    const long long lda = args.a.ld, ldb = args.b.ld;
+    const auto ra = make_rsrc(a, record_bytes(2 * (A_KMAJOR ? min(M, T::BM) * lda : K * lda)));
+    const auto rb = make_rsrc(b, record_bytes(2 * (B_KMAJOR ? min(N, T::BN) * ldb : K * ldb)));
+    phase_tile<T, A_KMAJOR, B_KMAJOR, ARGS::OUT, 0>(p, ra, rb, 0, M, N, K, 0, 0, p.t_n, a0, a1, bl0,
+                                                    bh0, bl1, bh1, stg);
+}
+
+template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
+__global__ __launch_bounds__(T::NT) void product_f32_kernel(ARGS args) {
+    __shared__ __attribute__((aligned(1024))) float lds[4 * T::OP_EL];
+    Tiled<ARGS> p;
+    const float *a, *b;
+    int M, N, K;
+    if (!place_tile<T, A_KMAJOR, B_KMAJOR>(args, &p, &a, &b, &M, &N, &K)) return;
+    f32_tile<T, A_KMAJOR, B_KMAJOR>(p, a, b, M, N, K, lds);
+}
+
+// ------------------------------------------------------------------ f32 main loop
+
+// One stage of an operand: 128 rows (or columns) by 16 k, two float4 a thread, zero
+// outside. k-major in LDS: 16-byte chunk c of row r at chunk c ^ (r / 4 mod 4);
+// mn-major: k row k, its columns XOR 32 (k / 4 mod 2), so that the halves of a wave
+// read other banks.
+template <bool KMAJOR>
+struct F32Stage {
+    float4 v[2];
+    __device__ __forceinline__ void load(const float* base, int ld, int lim, int k0, int K) {
+        const int tid = threadIdx.x;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            int mn, k;
+            if constexpr (KMAJOR) { mn = 64 * u + (tid >> 2); k = k0 + 4 * (tid & 3); }
+            else { mn = 4 * (tid & 31); k = k0 + 8 * u + (tid >> 5); }
+            v[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (mn < lim && k < K)
+                v[u] = *reinterpret_cast<const float4*>(
+                    base + (KMAJOR ? static_cast<size_t>(mn) * ld + k
+                                   : static_cast<size_t>(k) * ld + mn));
+        }
+    }
+    __device__ __forceinline__ void put(float* s) const {
+        const int tid = threadIdx.x;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (KMAJOR) {
+                const int r = 64 * u + (tid >> 2), c = tid & 3;
+                *reinterpret_cast<float4*>(s + r * 16 + ((c ^ ((r >> 2) & 3)) << 2)) = v[u];
+            } else {
+                const int k = 8 * u + (tid >> 5), c = 4 * (tid & 31);
+                *reinterpret_cast<float4*>(s + k * 128 + (c ^ (((k >> 2) & 1) << 5))) = v[u];
+            }
+        }
+    }
+    // four k of the lane's half (8 g + 4 (lane / 32) ..) of row mn0 + lane % 32
+    static __device__ __forceinline__ float4 frag(const float* s, int mn0, int g, int lane) {
+        const int mn = mn0 + (lane & 31), h = lane >> 5;
+        if constexpr (KMAJOR) {
+            return *reinterpret_cast<const float4*>(
+                s + mn * 16 + (((2 * g + h) ^ ((mn >> 2) & 3)) << 2));
+        } else {
+            const float* q = s + (8 * g + 4 * h) * 128 + (mn ^ (h << 5));
+            return make_float4(q[0], q[128], q[256], q[384]);
+        }
+    }
+};
+
+// v_mfma_f32_32x32x2f32 takes one k from either half of the lanes: of eight k, product t
+// multiplies k = t and 4 + t. Stages are double-buffered in LDS behind one barrier, the
+// next one's loads in flight in registers. Bound by the matrix instructions (64 cycles
+// each, 32 of them a stage and wave).
+template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
+__device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const float* b, int M,
+                                         int N, int K, float* lds) {
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int wm = wave / T::WGN, wn = wave % T::WGN;
+    const int fm_live = min(T::FM, max(0, (M - wm * T::WM + 31) / 32));
+    const bool row_sum = ARGS::OUT == EPI_F32 && p.bsum != nullptr && p.t_n == 0 && wn == 0;
+    f32x16 acc[T::FM][T::PB];
+    float rsum[T::FM];
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+        rsum[i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < T::PB; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+    }
+    F32Stage<A_KMAJOR> sa;
+    F32Stage<B_KMAJOR> sb;
+    // (mn-major columns come four at a time and the operands' rows are padded, so the
+    // last four may pass the limit: their outputs are not stored)
+    const int lim_a = min(M, T::BM), lim_b = min(N, T::BN);
+    sa.load(a, p.a.ld, lim_a, 0, K);
+    sb.load(b, p.b.ld, lim_b, 0, K);
+    for (int k0 = 0, buf = 0; k0 < K; k0 += T::KB, buf ^= 1) {
+        float* const as = lds + buf * 2 * T::OP_EL;
+        float* const bs = as + T::OP_EL;
+        sa.put(as);
+        sb.put(bs);
+        __syncthreads();
+        if (k0 + T::KB < K) {
+            sa.load(a, p.a.ld, lim_a, k0 + T::KB, K);
+            sb.load(b, p.b.ld, lim_b, k0 + T::KB, K);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            float4 fa[T::FM], fb[T::PB];
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i)
+                fa[i] = F32Stage<A_KMAJOR>::frag(as, 64 * wm + 32 * i, g, lane);
+#pragma unroll
+            for (int j = 0; j < T::PB; ++j)
+                fb[j] = F32Stage<B_KMAJOR>::frag(bs, 64 * j + 32 * wn, g, lane);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < T::FM; ++i) {
+                    const float av = t == 0 ? fa[i].x : t == 1 ? fa[i].y
+                                   : t == 2 ? fa[i].z : fa[i].w;
+                    if constexpr (ARGS::OUT == EPI_F32) rsum[i] += av;
+#pragma unroll
+                    for (int j = 0; j < T::PB; ++j) {
+                        const float bv = t == 0 ? fb[j].x : t == 1 ? fb[j].y
+                                       : t == 2 ? fb[j].z : fb[j].w;
+                        acc[i][j] =
+                            __builtin_amdgcn_mfma_f32_32x32x2f32(bv, av, acc[i][j], 0, 0, 0);
+                    }
+                }
+        }
+    }
+    __syncthreads();  // the stages are read: the outputs pass through their LDS
+    finish_tile(TileKind<T, ARGS::OUT>{}, p, acc, rsum, row_sum,
+                LdsArrays{nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
+                          reinterpret_cast<uint16_t*>(lds)},
+                0, M, N, 0, 0, fm_live);
+}
+
+// ------------------------------------------------------------------ tiles' outputs
+
+// Register 4 q + r of lane l, block i, panel b: row 64 wm + 32 i + l % 32, column
+// 64 b + 32 wn + 8 q + 4 (l / 32) + r of the tile.
+
+// z = product + bias in the accumulators; -infinity past the classes.
+template <class T>
+__device__ __forceinline__ void add_bias(f32x16 (&acc)[T::FM][T::PB], const float* zbias, int n0) {
+    const int lane = threadIdx.x & 63, wn = wave_id() % T::WGN;
+    const float* at = zbias + n0 + 32 * wn + 4 * (lane >> 5);
+#pragma unroll
+    for (int b = 0; b < T::PB; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float4 v = *reinterpret_cast<const float4*>(at + 64 * b + 8 * q);
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i) {
+                acc[i][b][4 * q] += v.x;
+                acc[i][b][4 * q + 1] += v.y;
+                acc[i][b][4 * q + 2] += v.z;
+                acc[i][b][4 * q + 3] += v.w;
+            }
+        }
+}
+
+// One 32 x 32 block of a wave's outputs to rows of `dst` (element type E), through LDS
+// of the wave's own: rows leave as 16-byte pieces, eight (f32) or four lanes a row.
+// Row r of the block goes to dst + r ld; rows from `rows` and columns from `cols`
+// (a multiple of 8 unless the row is padded beyond it) are left out. A wave's LDS
+// accesses run in order: no barrier.
+template <typename E>
+__device__ __forceinline__ void store_block(const f32x16& v, lds_u16* s, E* dst, size_t ld,
+                                            int rows, int cols) {
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const v4i32 w = __builtin_bit_cast(
+                v4i32, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
+            *reinterpret_cast<lds_v4*>(s + r * 64 + (((2 * q + h) ^ (r & 7)) << 3)) = w;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int rr = 8 * u + (lane >> 3), c = lane & 7;
+            const v4i32 w = *reinterpret_cast<lds_v4*>(s + rr * 64 + ((c ^ (rr & 7)) << 3));
+            if (rr < rows && 4 * c < cols) *reinterpret_cast<v4i32*>(dst + rr * ld + 4 * c) = w;
+        }
+    } else {
+        typedef int v2i32 __attribute__((ext_vector_type(2)));
+        typedef __attribute__((address_space(3))) v2i32 lds_v2;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<lds_v2*>(s + r * 32 + ((q ^ ((r >> 2) & 3)) << 3) + 4 * h) =
+                v2i32{static_cast<int>(pack_bf16x2(v[4 * q], v[4 * q + 1])),
+                      static_cast<int>(pack_bf16x2(v[4 * q + 2], v[4 * q + 3]))};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int rr = 16 * u + (lane >> 2), c = lane & 3;
+            const v4i32 w =
+                *reinterpret_cast<lds_v4*>(s + rr * 32 + ((c ^ ((rr >> 2) & 3)) << 3));
+            if (rr < rows && 8 * c < cols) *reinterpret_cast<v4i32*>(dst + rr * ld + 8 * c) = w;
+        }
+    }
+}
+
+// LDS of a wave's own, 4 KB.
+__device__ __forceinline__ lds_u16* wave_lds(const LdsArrays& arrays) {
+    return (lds_u16*)(arrays.b6) + wave_id() * 2048;
+}
+
+// Of each row and the wave's strip of columns: the largest z and the sum of
+// exp((z - that) / temperature).
+template <class T, int EPI>
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsArgs>& p,
+                                            f32x16 (&acc)[T::FM][T::PB], float (&)[T::FM], bool,
+                                            const LdsArrays&, int, int M, int, int, int,
+                                            int fm_live) {
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int wm = wave / T::WGN, wn = wave % T::WGN;
+    add_bias<T>(acc, p.zbias, p.t_n0);
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+        if (i >= fm_live) break;
+        float m = kLowest;
+#pragma unroll
+        for (int b = 0; b < T::PB; ++b)
+#pragma unroll
+            for (int c = 0; c < 16; ++c) m = fmaxf(m, acc[i][b][c]);
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        // (z - m first, exact where the two are near: with m scaled and rounded by itself
+        // the largest p would be off by its rounding)
+        auto total = [&](float scale) {
+            float s = 0.0f;
+#pragma unroll
+            for (int b = 0; b < T::PB; ++b)
+#pragma unroll
+                for (int c = 0; c < 16; ++c)
+                    s += __builtin_amdgcn_exp2f((acc[i][b][c] - m) * scale);
+            return s + __shfl_xor(s, 32, 64);
+        };
+        const int r = 64 * wm + 32 * i + lane;  // (lanes below 32)
+        const size_t at = static_cast<size_t>(p.t_n * T::WGN + wn) * p.n_rows + p.t_m0 + r;
+        const float s = total(p.scale);
+        const bool store = lane < 32 && r < M;
+        if (store) {
+            p.mx[at] = m;
+            p.sum[at] = s;
+        }
+        if (p.sum_t != nullptr) {
+            const float st = total(p.scale_t);
+            if (store) p.sum_t[at] = st;
+        }
+    }
+}
+
+// Weights of the two softmaxes in a row's dz.
+__device__ __forceinline__ float2 row_rates(const Header& h, const float2& weight, float w_label,
+                                            float w_teacher, int mean) {
+    float g = w_label * weight.x, t = w_teacher * weight.y;
+    if (mean) {
+        g = h.sum[0] != 0.0f ? g / h.sum[0] : 0.0f;
+        t = h.sum[1] != 0.0f ? t / h.sum[1] : 0.0f;
+    }
+    return make_float2(g, t);
+}
+
+// One softmax or two at logit z of a row, times their weights g: see Saved::rec.
+struct Softmax {
+    bool two;
+    float scale, scale_t;
+    __device__ __forceinline__ Softmax(const Header& h, int teacher, float inv_t)
+        : two(teacher && h.labelled && inv_t != 1.0f),
+          scale(kLog2e * (teacher && !h.labelled ? inv_t : 1.0f)), scale_t(kLog2e * inv_t) {}
+    template <bool TWO>
+    __device__ __forceinline__ float at(float z, const float4& rec, const float2& g) const {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z - rec.x, scale, -rec.y));
+        if constexpr (!TWO) return (g.x + g.y) * p;
+        const float pt = __builtin_amdgcn_exp2f(__builtin_fmaf(z - rec.x, scale_t, -rec.z));
+        return __builtin_fmaf(g.x, p, g.y * pt);
+    }
+};
+
+// dz without its targets. One softmax serves both losses where the temperature is 1 or
+// only one of them is there.
+template <class T, int EPI>
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<GradZArgs>& p,
+                                            f32x16 (&acc)[T::FM][T::PB], float (&)[T::FM], bool,
+                                            const LdsArrays& arrays, int, int M, int, int, int,
+                                            int fm_live) {
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int wm = wave / T::WGN, wn = wave % T::WGN;
+    const Header h = *p.head;
+    const Softmax soft(h, p.teacher, p.inv_t);
+    add_bias<T>(acc, p.zbias, p.t_n0);
+    Elm<T>* const dz = static_cast<Elm<T>*>(p.dz);
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+        if (i >= fm_live) break;
+        const int r0 = 64 * wm + 32 * i, r = p.t_m0 + min(r0 + (lane & 31), M - 1);
+        const float4 rec = p.rec[r];
+        const float2 g = row_rates(h, p.weight[r], p.w_label, p.w_teacher, p.mean);
+#pragma unroll
+        for (int b = 0; b < T::PB; ++b) {
+            f32x16 v;
+            if (soft.two) {
+#pragma unroll
+                for (int c = 0; c < 16; ++c) v[c] = soft.at<true>(acc[i][b][c], rec, g);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 16; ++c) v[c] = soft.at<false>(acc[i][b][c], rec, g);
+            }
+            const int n = p.t_n0 + 64 * b + 32 * wn;
+            store_block(v, wave_lds(arrays), dz + static_cast<size_t>(p.t_m0 + r0) * p.ldz + n,
+                        p.ldz, M - r0, p.ldz - n);
+        }
+    }
+}
+
+// f32 sums of the tile's range of k, into its slot.
+template <class T, int EPI>
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<PartArgs>& p,
+                                            f32x16 (&acc)[T::FM][T::PB], float (&rsum)[T::FM],
+                                            bool row_sum, const LdsArrays& arrays, int, int M,
+                                            int N, int, int, int fm_live) {
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int wm = wave / T::WGN, wn = wave % T::WGN;
+    float* const part = p.part + p.t_split * p.part_stride;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+        if (i >= fm_live) break;
+        const int r0 = 64 * wm + 32 * i;
+        if (row_sum) {
+            const float t = rsum[i] + __shfl_xor(rsum[i], 32, 64);
+            if (lane < 32 && r0 + lane < M)
+                p.part_sums[static_cast<size_t>(p.t_split) * p.M + p.t_m0 + r0 + lane] = t;
+        }
+#pragma unroll
+        for (int b = 0; b < T::PB; ++b) {
+            const int n = 64 * b + 32 * wn;
+            if (n >= N) break;
+            float* const at = part + static_cast<size_t>(p.t_m0 + r0) * p.N + p.t_n0 + n;
+            f32x16 v = acc[i][b];
+            if (p.add) {
+                const int r = lane & 31;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = 8 * q + 4 * (lane >> 5);
+                    if (r0 + r < M && n + c < N) {
+                        const float4 o = *reinterpret_cast<const float4*>(
+                            at + static_cast<size_t>(r) * p.N + c);
+                        v[4 * q] += o.x;
+                        v[4 * q + 1] += o.y;
+                        v[4 * q + 2] += o.z;
+                        v[4 * q + 3] += o.w;
+                    }
+                }
+            }
+            store_block(v, wave_lds(arrays), at, p.N, M - r0, N - n);
+        }
+    }
+}
+
+// The product rounded to its type.
+template <class T, int EPI>
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StoreArgs>& p,
+                                            f32x16 (&acc)[T::FM][T::PB], float (&rsum)[T::FM],
+                                            bool row_sum, const LdsArrays& arrays, int, int M,
+                                            int N, int, int, int fm_live) {
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int wm = wave / T::WGN, wn = wave % T::WGN;
+    Elm<T>* const c = static_cast<Elm<T>*>(p.c);
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+        if (i >= fm_live) break;
+        const int r0 = 64 * wm + 32 * i;
+        if (row_sum) {
+            const float t = rsum[i] + __shfl_xor(rsum[i], 32, 64);
+            if (lane < 32 && r0 + lane < M)
+                Elem<Elm<T>>::store(static_cast<Elm<T>*>(p.sums), p.t_m0 + r0 + lane, t);
+        }
+        if (c == nullptr) continue;
+#pragma unroll
+        for (int b = 0; b < T::PB; ++b) {
+            const int n = 64 * b + 32 * wn;
+            if (n >= N) break;
+            store_block(acc[i][b], wave_lds(arrays),
+                        c + static_cast<size_t>(p.t_m0 + r0) * p.N + p.t_n0 + n, p.N, M - r0,
+                        N - n);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ rows
+
+__device__ __forceinline__ bool is_class(int c, int V) { return c >= 0 && c < V; }
+
+struct MarkArgs {
+    const void* bias;
+    const int32_t* labels;
+    const int32_t* teacher_idx;
+    const float* teacher_logits;
+    const float* row_weight;
+    float* row_losses;
+    int32_t* place;   // of live rows: the place among the block's
+    int32_t* counts;  // [row blocks] live rows
+    float* zbias;
+    unsigned* ticket;
+    int N, V, K, vpad, row_blocks, dtype;
+};
+
+// Blocks [0, row_blocks): a row a thread; the others the bias.
+__global__ __launch_bounds__(kMarkRows) void mark_kernel(MarkArgs p) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
+        const int c = (blockIdx.x - p.row_blocks) * kMarkRows + tid;
+        if (c == 0) *p.ticket = 0;
+        if (c >= p.vpad) return;
+        float v = -__builtin_inff();
+        if (c < p.V) {
+            v = 0.0f;
+            if (p.bias != nullptr)
+                v = p.dtype == VMOE_BF16 ? bf16_to_f32(static_cast<const uint16_t*>(p.bias)[c])
+                                         : static_cast<const float*>(p.bias)[c];
+        }
+        p.zbias[c] = v;
+        return;
+    }
+    __shared__ int wsum[kMarkRows / 64];
+    const int t = blockIdx.x * kMarkRows + tid;
+    bool live = false;
+    if (t < p.N && (p.row_weight == nullptr || p.row_weight[t] != 0.0f)) {
+        live = p.labels != nullptr && is_class(p.labels[t], p.V);
+        const size_t at = static_cast<size_t>(t) * p.K;
+        for (int j = 0; j < p.K && !live; ++j)
+            live = is_class(p.teacher_idx[at + j], p.V) &&
+                   p.teacher_logits[at + j] != -__builtin_inff();
+    }
+    const uint64_t all = __ballot(live);
+    if (lane == 0) wsum[wave] = __popcll(all);
+    __syncthreads();
+    int before = __popcll(all & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) before += wsum[w];
+    if (t < p.N) {
+        p.place[t] = live ? before : -1;
+        if (!live && p.row_losses != nullptr)
+            reinterpret_cast<float2*>(p.row_losses)[t] = make_float2(0.0f, 0.0f);
+    }
+    if (tid == kMarkRows - 1) p.counts[blockIdx.x] = before + (live ? 1 : 0);
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+
+// Between a wave's LDS writes and its reads of what other lanes wrote (LDS accesses of
+// one wave run in order: only the compiler is held).
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0];
+    const float4 b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        v[2 * q] = bf16_to_f32(w[q] & 0xFFFFu);
+        v[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u);
+    }
+}
+
+struct RowArgs {
+    const void* x;
+    const int32_t* labels;
+    const int32_t* teacher_idx;
+    const float* teacher_logits;
+    const float* row_weight;
+    const int32_t* counts;
+    Saved s;
+    int N, V, K, d, row_blocks;
+    float inv_t;
+};
+
+// Rows 4 b .. + 3 of block b, a wave each.
+template <typename E>
+__global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
+    constexpr int R = (VMOE_HEAD_MAX_TEACHER + 63) / 64;  // entries a lane
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int t = blockIdx.x * 4 + wave, mine = blockIdx.x * 4 / kMarkRows;
+    auto live_before = [&](int blocks) {
+        int n = 0;
+        for (int b = lane; b < blocks; b += 64) n += p.counts[b];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+        return n;
+    };
+    if (blockIdx.x == 0 && wave == 0) {
+        const int all = live_before(p.row_blocks);
+        if (lane == 0) {
+            p.s.head->live = all;
+            p.s.head->labelled = p.labels != nullptr;
+        }
+    }
+    if (t >= p.N) return;
+    const int local = p.s.place[t];
+    if (local < 0) return;
+    const int at = local + live_before(mine);
+    const E* const x = static_cast<const E*>(p.x) + static_cast<size_t>(t) * p.d;
+    E* const xc = static_cast<E*>(p.s.x) + static_cast<size_t>(at) * p.d;
+    constexpr int PER = 16 / sizeof(E);
+    for (int c = lane * PER; c < p.d; c += 64 * PER)
+        *reinterpret_cast<uint4*>(xc + c) = *reinterpret_cast<const uint4*>(x + c);
+
+    const size_t out = static_cast<size_t>(at) * (1 + p.K);
+    const int label = p.labels != nullptr ? p.labels[t] : -1;
+    const bool labelled = is_class(label, p.V);
+    int idx[R];
+    float u[R];  // the entries' logits
+    float top = -__builtin_inff();
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = lane + 64 * i;
+        idx[i] = -1;
+        u[i] = 0.0f;
+        if (j < p.K) {
+            const size_t from = static_cast<size_t>(t) * p.K + j;
+            const int c = p.teacher_idx[from];
+            if (is_class(c, p.V)) {
+                u[i] = p.teacher_logits[from];
+                if (u[i] != -__builtin_inff()) {
+                    idx[i] = c;
+                    top = fmaxf(top, u[i]);
+                    any = true;
+                }
+            }
+        }
+    }
+    const bool taught = __any(any);
+    float mass = 0.0f, inner = 0.0f;
+    if (taught) {  // uniform
+        top = wave_max(top);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            // (the difference first: logits near the largest f32 stay finite)
+            u[i] = (u[i] - top) * p.inv_t;
+            mass += idx[i] >= 0 ? __expf(u[i]) : 0.0f;
+        }
+        mass = wave_total(mass);
+    }
+    const float log_mass = logf(mass);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int j = lane + 64 * i;
+        float q = 0.0f;
+        if (idx[i] >= 0) {
+            q = __expf(u[i]) / mass;
+            // (an entry too small to count: not 0 times its logarithm, infinite at worst)
+            if (q != 0.0f) inner += q * (u[i] - log_mass);
+        }
+        if (j < p.K) {
+            p.s.tidx[out + 1 + j] = idx[i];
+            p.s.tq[out + 1 + j] = q;
+        }
+    }
+    inner = wave_total(inner);
+    if (lane == 0) {
+        const float w = p.row_weight != nullptr ? p.row_weight[t] : 1.0f;
+        p.s.tidx[out] = labelled ? label : -1;
+        p.s.tq[out] = labelled ? 1.0f : 0.0f;
+        p.s.row[at] = t;
+        p.s.rec[at] = make_float4(0.0f, 0.0f, 0.0f, inner);
+        p.s.weight[at] = make_float2(labelled ? w : 0.0f, taught ? w : 0.0f);
+        p.s.place[t] = at;
+    }
+}
+
+struct TargetArgs {
+    Saved s;
+    const void* weight;
+    int K, d;
+};
+
+// Logits of the rows' targets, 32 pairs of a row and a class a wave: the diagonal of
+// the pairs' 32 x 32 product. The other products are thrown away, but the sums have
+// the bits of the tiles' (the same instructions on the same k, in order), which p - 1
+// and p - q need where they are small: a sum in another order, off by 1e-6 at logits
+// of 14, left 1 - p of a row that is nearly certain with three digits.
+template <typename E>
+__global__ __launch_bounds__(256) void targets_kernel(TargetArgs p) {
+    const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
+    const long long first = 32LL * (4LL * blockIdx.x + wave);
+    const int n = 1 + p.K;
+    const long long pairs = static_cast<long long>(p.s.head->live) * n;
+    if (first >= pairs) return;
+    const long long pair = first + (lane & 31);
+    const bool in = pair < pairs;
+    const int c = in ? p.s.tidx[pair] : -1;
+    if (!__any(c >= 0)) {
+        if (in && h == 0) p.s.tz[pair] = 0.0f;
+        return;
+    }
+    const E* const w = static_cast<const E*>(p.weight) + static_cast<size_t>(max(c, 0)) * p.d;
+    const E* const x = static_cast<const E*>(p.s.x) + static_cast<size_t>(in ? pair / n : 0) * p.d;
+    f32x16 acc;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
+    if constexpr (sizeof(E) == 2) {
+        constexpr int U = 8;  // steps of 16 k in flight
+        for (int k0 = 0; k0 < p.d; k0 += 16 * U) {
+            uint4 fw[U], fx[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = k0 + 16 * u + 8 * h;
+                fw[u] = fx[u] = make_uint4(0u, 0u, 0u, 0u);
+                if (k < p.d) {
+                    fw[u] = *reinterpret_cast<const uint4*>(w + k);
+                    fx[u] = *reinterpret_cast<const uint4*>(x + k);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8, fw[u]), __builtin_bit_cast(bf16x8, fx[u]), acc, 0, 0,
+                    0);
+        }
+    } else {
+        constexpr int U = 8;  // steps of 8 k in flight
+        for (int k0 = 0; k0 < p.d; k0 += 8 * U) {
+            float4 fw[U], fx[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = k0 + 8 * u + 4 * h;
+                fw[u] = fx[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (k < p.d) {
+                    fw[u] = *reinterpret_cast<const float4*>(w + k);
+                    fx[u] = *reinterpret_cast<const float4*>(x + k);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fw[u].x, fx[u].x, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fw[u].y, fx[u].y, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fw[u].z, fx[u].z, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fw[u].w, fx[u].w, acc, 0, 0, 0);
+            }
+        }
+    }
+    // register 4 q + r of lane l: class 8 q + 4 (l / 32) + r against row l % 32
+    const int j = lane & 31;
+    float z = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (8 * q + 4 * h + r == j) z = acc[4 * q + r];
+    if (((j >> 2) & 1) == h && in) p.s.tz[pair] = c >= 0 ? z + p.s.bias[c] : 0.0f;
+}
+
+struct FinishArgs {
+    Saved s;
+    const float *mx, *sum, *sum_t;
+    double* sums;  // [blocks][4]
+    unsigned* ticket;
+    float *losses, *row_losses;
+    int strips, N, K, mean;
+    float temperature, inv, inv_t;  // inv: of `sum`'s softmax
+};
+
+constexpr int kFinishWaves = 8;
+
+// 64 live rows a block, a lane each; the waves share the strips.
+__global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p) {
+    // max z / T and z / T of a target are to be rounded alike: their difference counts
+#pragma clang fp contract(off)
+    constexpr int W = kFinishWaves;
+    __shared__ float mx_s[W][64], sum_s[W][64], sumt_s[W][64], cross_s[W][64];
+    __shared__ double part_s[W][4];
+    __shared__ bool last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int live = p.s.head->live;
+    const int r = blockIdx.x * 64 + lane;
+    const bool in = r < live;
+    auto join = [&](float& m, float& s, float& st, float m2, float s2, float st2) {
+        const float top = fmaxf(m, m2);
+        const float scale = kLog2e * p.inv, scale_t = kLog2e * p.inv_t;
+        const float a = (m - top) * scale, b = (m2 - top) * scale;
+        s = s * __builtin_amdgcn_exp2f(a) + s2 * __builtin_amdgcn_exp2f(b);
+        if (p.sum_t != nullptr) {
+            const float at = (m - top) * scale_t, bt = (m2 - top) * scale_t;
+            st = st * __builtin_amdgcn_exp2f(at) + st2 * __builtin_amdgcn_exp2f(bt);
+        }
+        m = top;
+    };
+    float m = kLowest, s = 0.0f, st = 0.0f, cross = 0.0f;
+    if (in) {
+        const size_t entry = static_cast<size_t>(r) * (1 + p.K);
+        for (int j = 1 + wave; j <= p.K; j += W)  // (z of an entry that is none is 0)
+            cross = __builtin_fmaf(p.s.tq[entry + j], p.s.tz[entry + j] * p.inv_t, cross);
+        for (int q = wave; q < p.strips; q += W) {
+            const size_t at = static_cast<size_t>(q) * p.N + r;
+            join(m, s, st, p.mx[at], p.sum[at], p.sum_t != nullptr ? p.sum_t[at] : 0.0f);
+        }
+    }
+    mx_s[wave][lane] = m;
+    sum_s[wave][lane] = s;
+    sumt_s[wave][lane] = st;
+    cross_s[wave][lane] = cross;
+    __syncthreads();
+    if (wave == 0) {
+        double v[4] = {0.0, 0.0, 0.0, 0.0};
+        if (in) {
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                join(m, s, st, mx_s[w][lane], sum_s[w][lane], sumt_s[w][lane]);
+                cross += cross_s[w][lane];
+            }
+            if (p.sum_t == nullptr) st = s;
+            const float2 weight = p.s.weight[r];
+            float4 rec = p.s.rec[r];
+            // (a live row's weight is not 0)
+            const bool label = weight.x != 0.0f, taught = weight.y != 0.0f;
+            const float lse = m * p.inv + logf(s), lse_t = m * p.inv_t + logf(st);
+            const float a =
+                label ? lse - p.s.tz[static_cast<size_t>(r) * (1 + p.K)] : 0.0f;
+            const float tt = p.temperature * p.temperature;
+            const float b = taught ? tt * ((rec.w - cross) + lse_t) : 0.0f;
+            rec.x = m;
+            rec.y = log2f(s);
+            rec.z = log2f(st);
+            p.s.rec[r] = rec;
+            if (p.row_losses != nullptr)
+                reinterpret_cast<float2*>(p.row_losses)[p.s.row[r]] = make_float2(a, b);
+            v[0] = static_cast<double>(weight.x) * a;
+            v[1] = static_cast<double>(weight.y) * b;
+            v[2] = weight.x;
+            v[3] = weight.y;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) v[c] += __shfl_xor(v[c], o, 64);
+        }
+        if (lane == 0) {
+            // (agent scope: the last block may run on another XCD)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                __hip_atomic_store(p.sums + 4 * blockIdx.x + c, v[c], __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+            last = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_ACQ_REL,
+                                          __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        }
+    }
+    __syncthreads();
+    if (!last) return;
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+    const int blocks = min(static_cast<int>(gridDim.x), (live + 63) / 64);
+    for (int q = tid; q < blocks; q += 64 * W)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            v[c] += __hip_atomic_load(p.sums + 4 * q + c, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) v[c] += __shfl_xor(v[c], o, 64);
+        if (lane == 0) part_s[wave][c] = v[c];
+    }
+    __syncthreads();
+    if (tid < 2) {
+        double a = 0.0, n = 0.0;
+        for (int w = 0; w < W; ++w) {
+            a += part_s[w][tid];
+            n += part_s[w][2 + tid];
+        }
+        if (p.mean) a = n != 0.0 ? a / n : 0.0;
+        p.losses[tid] = static_cast<float>(a);
+        p.losses[2 + tid] = static_cast<float>(n);
+        p.s.head->sum[tid] = static_cast<float>(n);
+    }
+}
+
+struct SubtractArgs {
+    Saved s;
+    void* dz;
+    int ldz, first, count;  // the piece's classes
+    int K, mean, teacher;
+    float w_label, w_teacher, inv_t;
+};
+
+// dz at a row's targets: a wave a row, a lane an entry. Entries of one class (a label
+// among the teacher's) write the same value, which each of them sums in the same order.
+template <typename E>
+__global__ __launch_bounds__(256) void subtract_kernel(SubtractArgs p) {
+    __shared__ int idx_s[4][VMOE_HEAD_MAX_TEACHER + 1];
+    __shared__ float q_s[4][VMOE_HEAD_MAX_TEACHER + 1];
+    const int lane = threadIdx.x & 63, wave = wave_id(), r = blockIdx.x * 4 + wave;
+    const Header h = *p.s.head;
+    if (r >= h.live) return;
+    const int n = 1 + p.K;
+    const size_t at = static_cast<size_t>(r) * n;
+    const float4 rec = p.s.rec[r];
+    const float2 g = row_rates(h, p.s.weight[r], p.w_label, p.w_teacher, p.mean);
+    for (int e = lane; e < n; e += 64) {
+        idx_s[wave][e] = p.s.tidx[at + e];
+        q_s[wave][e] = e == 0 ? g.x : g.y * p.s.tq[at + e];
+    }
+    wave_lds_fence();
+    const Softmax soft(h, p.teacher, p.inv_t);
+    E* const dz = static_cast<E*>(p.dz) + static_cast<size_t>(r) * p.ldz;
+    for (int e = lane; e < n; e += 64) {
+        const int c = idx_s[wave][e];
+        if (c < p.first || c >= p.first + p.count) continue;
+        const float z = p.s.tz[at + e];
+        const float v = soft.two ? soft.at<true>(z, rec, g) : soft.at<false>(z, rec, g);
+        float hit = 0.0f;
+        for (int o = 0; o < n; ++o) hit += idx_s[wave][o] == c ? q_s[wave][o] : 0.0f;
+        Elem<E>::store(dz, c - p.first, v - hit);
+    }
+}
+
+// dx: the slots' sums, rounded, to the rows' places; zeros for rows left out. Eight
+// columns a thread.
+template <typename E>
+__global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ part, size_t stride,
+                                                 int slots, const int32_t* __restrict__ place,
+                                                 E* __restrict__ dx, int N, int d) {
+    const int per = d / 8;
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= static_cast<long long>(N) * per) return;
+    const int t = static_cast<int>(i / per), c = 8 * static_cast<int>(i % per), r = place[t];
+    float v[8] = {};
+    if (r >= 0) {
+        const float* at = part + static_cast<size_t>(r) * d + c;
+        for (int s = 0; s < slots; ++s) {
+            float w[8];
+            load8(at + s * stride, w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] += w[q];
+        }
+    }
+    E* const out = dx + static_cast<size_t>(t) * d + c;
+    if constexpr (sizeof(E) == 4) {
+        reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        *reinterpret_cast<uint4*>(out) =
+            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                       pack_bf16x2(v[6], v[7]));
+    }
+}
+
+// dW and db of a piece from the slots of its ranges of rows.
+template <typename E>
+__global__ __launch_bounds__(256) void dw_kernel(const float* __restrict__ part, size_t stride,
+                                                 const float* __restrict__ part_sums, int slots,
+                                                 E* __restrict__ dw, E* __restrict__ db, int M,
+                                                 int d) {
+    const int per = d / 8;
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    if (db != nullptr && i < M) {
+        float v = 0.0f;
+        for (int s = 0; s < slots; ++s) v += part_sums[static_cast<size_t>(s) * M + i];
+        Elem<E>::store(db, i, v);
+    }
+    if (i >= static_cast<long long>(M) * per) return;
+    float v[8] = {};
+    for (int s = 0; s < slots; ++s) {
+        float w[8];
+        load8(part + s * stride + 8 * i, w);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] += w[q];
+    }
+    E* const out = dw + 8 * i;
+    if constexpr (sizeof(E) == 4) {
+        reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        *reinterpret_cast<uint4*>(out) =
+            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                       pack_bf16x2(v[6], v[7]));
+    }
+}
+
+// ------------------------------------------------------------------ launches
+
+// How a product over M x N with k in `stages` of 64 is cut: the tile's width and the
+// ranges of k.
+struct Cut {
+    int narrow, splits;
+};
+
+// Time of a cut in units of one CU's 64-deep stage of a 256 x 256 tile (1.8 us): rounds
+// of a tile a CU, each its stages and `extra` for its start and its outputs; more than
+// one range also writes and reads f32 sums (0.06 a tile and range).
+double cut_cost(long long tiles, int stages, int splits, double width, double extra) {
+    const long long rounds = (tiles * splits + kCus - 1) / kCus;
+    const double part = splits > 1 ? 0.06 * width * static_cast<double>(tiles) * splits : 0.0;
+    return static_cast<double>(rounds) * width * ((stages + splits - 1) / splits + extra) + part;
+}
+
+Cut choose_cut(const vmoe_head_shape& s, long long M, long long N, long long K, int max_splits) {
+    Cut best{0, 1};
+    if (s.dtype != VMOE_BF16) {
+        // 128 x 128, two blocks a CU: four of them for a 256 x 256 tile
+        const long long tiles = ((M + 127) / 128 * ((N + 127) / 128) + 1) / 2;
+        const int stages = static_cast<int>((K + 63) / 64);
+        double least = 1e300;
+        for (int sp = 1; sp <= max_splits && sp <= stages; sp *= 2) {
+            const double c = cut_cost(tiles, stages, sp, 0.5, 1.0);
+            if (c < least) {
+                least = c;
+                best.splits = sp;
+            }
+        }
+        return best;
+    }
+    const long long tm = (M + 255) / 256;
+    const int stages = static_cast<int>((K + 63) / 64);
+    double least = 1e300;
+    for (int narrow = 0; narrow < 2; ++narrow) {
+        const int bn = narrow ? 192 : 256;
+        const double width = narrow ? 0.75 * 1.05 : 1.0;
+        for (int sp = 1; sp <= max_splits && sp <= (stages > 0 ? stages : 1); ++sp) {
+            const double c = cut_cost(tm * ((N + bn - 1) / bn), stages, sp, width, 8.0);
+            if (c < least) {
+                least = c;
+                best = Cut{narrow, sp};
+            }
+        }
+    }
+    return best;
+}
+
+constexpr int kMaxDxSplits = 64, kMaxDwSplits = 16;
+
+// The backward's pieces of the classes, and its workspace.
+struct Plan {
+    int cols, pieces;  // classes a piece (a multiple of 256)
+    Cut dx, dw;        // of a whole piece
+    size_t dz_off, dx_off, dw_off, sums_off, bytes;
+};
+
+Plan make_plan(const vmoe_head_shape& s) {
+    Plan p;
+    const long long N = s.n_rows > 0 ? s.n_rows : 1, d = s.d_model;
+    const long long vpad = padded_classes(s);
+    long long cols = static_cast<long long>(kPieceBytes / (N * elem_bytes(s))) / 256 * 256;
+    // (a piece's rows of weight stay within 32-bit offsets)
+    const long long wcols = ((1LL << 30) - 1) / d / 256 * 256;
+    cols = cols < wcols ? cols : wcols;
+    cols = cols < 256 ? 256 : cols;
+    p.pieces = static_cast<int>((vpad + cols - 1) / cols);
+    p.cols = static_cast<int>(up256((vpad + p.pieces - 1) / p.pieces));
+    p.dx = choose_cut(s, N, d, p.cols, kMaxDxSplits);
+    p.dw = choose_cut(s, p.cols, d, N, kMaxDwSplits);
+    Carver c{nullptr};
+    auto take = [&](size_t bytes) {
+        const size_t at = c.off;
+        c.take<char>(bytes);
+        return at;
+    };
+    p.dz_off = take(static_cast<size_t>(N) * p.cols * elem_bytes(s));
+    p.dx_off = take(4 * static_cast<size_t>(p.dx.splits) * N * d);
+    p.dw_off = take(p.dw.splits > 1 ? 4 * static_cast<size_t>(p.dw.splits) * p.cols * d : 0);
+    p.sums_off = take(p.dw.splits > 1 ? 4 * static_cast<size_t>(p.dw.splits) * p.cols : 0);
+    p.bytes = c.off;
+    return p;
+}
+
+template <class T>
+int strips_of(const vmoe_head_shape& s) {
+    return static_cast<int>(cdiv(s.n_classes, T::BN)) * T::WGN;
+}
+
+struct FwdPlan {
+    int row_blocks, strips, finish_blocks, two;
+    size_t counts_off, ticket_off, sums_off, mx_off, sum_off, sumt_off, bytes;
+};
+
+FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
+    FwdPlan p;
+    const size_t N = s.n_rows;
+    p.row_blocks = static_cast<int>(cdiv(s.n_rows, kMarkRows));
+    p.strips = s.dtype == VMOE_BF16 ? strips_of<TileBig>(s) : strips_of<F32Tile>(s);
+    p.finish_blocks = s.n_rows > 0 ? static_cast<int>(cdiv(s.n_rows, 64)) : 1;
+    p.two = labels && s.n_teacher > 0 && s.temperature != 1.0f;
+    Carver c{nullptr};
+    auto take = [&](size_t bytes) {
+        const size_t at = c.off;
+        c.take<char>(bytes);
+        return at;
+    };
+    p.counts_off = take(4 * static_cast<size_t>(p.row_blocks));
+    p.ticket_off = take(4);
+    p.sums_off = take(32 * static_cast<size_t>(p.finish_blocks));
+    p.mx_off = take(4 * N * p.strips);
+    p.sum_off = take(4 * N * p.strips);
+    p.sumt_off = take(p.two ? 4 * N * p.strips : 0);
+    p.bytes = c.off;
+    return p;
+}
+
+template <class T, bool AK, bool BK, class ARGS>
+void launch_product(ARGS a, long long grid_m, hipStream_t st) {
+    a.tiles_n = static_cast<int>(cdiv(a.N, T::BN));
+    a.group_m = 4;
+    a.chunk = 16;
+    const long long tiles = static_cast<long long>(cdiv(grid_m, T::BM)) * a.tiles_n * a.splits;
+    if (tiles == 0) return;
+    const unsigned grid = 8 * cdiv(tiles, 8 * a.chunk) * a.chunk;
+    if constexpr (is_f32<T>())
+        product_f32_kernel<T, AK, BK><<<grid, T::NT, 0, st>>>(a);
+    else
+        product_bf16_kernel<T, AK, BK><<<grid, T::NT, 0, st>>>(a);
+}
+
+template <bool AK, bool BK, class ARGS>
+void launch_product(const vmoe_head_shape& s, int narrow, const ARGS& a, long long grid_m,
+                    hipStream_t st) {
+    if (s.dtype != VMOE_BF16) launch_product<F32Tile, AK, BK>(a, grid_m, st);
+    else if (narrow) launch_product<TileNarrow, AK, BK>(a, grid_m, st);
+    else launch_product<TileBig, AK, BK>(a, grid_m, st);
+}
+
+}  // namespace
+
+size_t head_saved_bytes(const vmoe_head_shape& s) { return saved_layout(s, nullptr).bytes; }
+size_t head_fwd_workspace_bytes(const vmoe_head_shape& s) { return make_fwd_plan(s, true).bytes; }
+size_t head_bwd_workspace_bytes(const vmoe_head_shape& s) { return make_plan(s).bytes; }
+
+vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void* weight,
+                            const void* bias, const int32_t* labels, const int32_t* teacher_idx,
+                            const float* teacher_logits, const float* row_weight, float* losses,
+                            float* row_losses, void* saved, void* ws, hipStream_t st) {
+    const Saved v = saved_layout(s, saved);
+    const FwdPlan p = make_fwd_plan(s, labels != nullptr);
+    char* const base = static_cast<char*>(ws);
+    const int N = s.n_rows, V = s.n_classes, K = s.n_teacher;
+    MarkArgs m{bias, labels, teacher_idx, teacher_logits, row_weight, row_losses, v.place,
+               reinterpret_cast<int32_t*>(base + p.counts_off), v.bias,
+               reinterpret_cast<unsigned*>(base + p.ticket_off), N, V, K, padded_classes(s),
+               p.row_blocks, s.dtype};
+    mark_kernel<<<p.row_blocks + cdiv(padded_classes(s), kMarkRows), kMarkRows, 0, st>>>(m);
+    const float inv_t = 1.0f / s.temperature;
+    const RowArgs t{x, labels, teacher_idx, teacher_logits, row_weight, m.counts, v,
+                    N, V, K, s.d_model, p.row_blocks, inv_t};
+    const unsigned row_grid = N > 0 ? cdiv(N, 4) : 1;
+    const TargetArgs g{v, weight, K, s.d_model};
+    const unsigned pair_grid = cdiv(static_cast<long long>(N) * (1 + K), 128);
+    if (s.dtype == VMOE_BF16) {
+        rows_kernel<uint16_t><<<row_grid, 256, 0, st>>>(t);
+        if (N > 0) targets_kernel<uint16_t><<<pair_grid, 256, 0, st>>>(g);
+    } else {
+        rows_kernel<float><<<row_grid, 256, 0, st>>>(t);
+        if (N > 0) targets_kernel<float><<<pair_grid, 256, 0, st>>>(g);
+    }
+
+    StatsArgs a{};
+    a.a = Operand{v.x, 0, s.d_model};
+    a.b = Operand{weight, 0, s.d_model};
+    a.M = N;
+    a.N = V;
+    a.K = s.d_model;
+    a.live = &v.head->live;
+    a.splits = 1;
+    a.zbias = v.bias;
+    a.mx = reinterpret_cast<float*>(base + p.mx_off);
+    a.sum = reinterpret_cast<float*>(base + p.sum_off);
+    a.sum_t = p.two ? reinterpret_cast<float*>(base + p.sumt_off) : nullptr;
+    a.n_rows = N;
+    a.scale_t = kLog2e * inv_t;
+    a.scale = K > 0 && labels == nullptr ? a.scale_t : kLog2e;
+    launch_product<true, true>(s, 0, a, N, st);
+
+    const FinishArgs f{v, a.mx, a.sum, a.sum_t,
+                       reinterpret_cast<double*>(base + p.sums_off), m.ticket,
+                 losses, row_losses, p.strips, N, K, s.reduction == VMOE_REDUCE_MEAN,
+                 s.temperature, K > 0 && labels == nullptr ? inv_t : 1.0f, inv_t};
+    finish_kernel<<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
+    return launch_status();
+}
+
+vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const void* saved,
+                            float w_label, float w_teacher, void* dx, void* dweight, void* dbias,
+                            void* ws, hipStream_t st) {
+    const Saved v = saved_layout(s, const_cast<void*>(saved));
+    const Plan p = make_plan(s);
+    char* const base = static_cast<char*>(ws);
+    const int N = s.n_rows, V = s.n_classes, d = s.d_model;
+    const size_t size = elem_bytes(s);
+    const bool bf16 = s.dtype == VMOE_BF16;
+    const bool params = dweight != nullptr || dbias != nullptr;
+    for (int i = 0; i < p.pieces; ++i) {
+        const int first = i * p.cols, count = min(p.cols, V - first);
+        if (count <= 0) break;
+        const char* const w =
+            static_cast<const char*>(weight) + static_cast<size_t>(first) * d * size;
+        GradZArgs z{};
+        z.a = Operand{v.x, 0, d};
+        z.b = Operand{w, 0, d};
+        z.M = N;
+        z.N = count;
+        z.K = d;
+        z.live = &v.head->live;
+        z.splits = 1;
+        z.zbias = v.bias + first;
+        z.head = v.head;
+        z.rec = v.rec;
+        z.weight = v.weight;
+        z.dz = base + p.dz_off;
+        z.ldz = static_cast<int>(up256(count));
+        z.w_label = w_label;
+        z.w_teacher = w_teacher * s.temperature;
+        z.inv_t = 1.0f / s.temperature;
+        z.mean = s.reduction == VMOE_REDUCE_MEAN;
+        z.teacher = s.n_teacher > 0;
+        launch_product<true, true>(s, 0, z, N, st);
+        if (N > 0) {
+            const SubtractArgs u{v, z.dz, z.ldz, first, count, s.n_teacher, z.mean, z.teacher,
+                                 z.w_label, z.w_teacher, z.inv_t};
+            if (bf16) subtract_kernel<uint16_t><<<cdiv(N, 4), 256, 0, st>>>(u);
+            else subtract_kernel<float><<<cdiv(N, 4), 256, 0, st>>>(u);
+        }
+        if (dx != nullptr) {
+            PartArgs a{};
+            a.a = Operand{z.dz, 0, z.ldz};
+            a.b = Operand{w, 0, d};
+            a.M = N;
+            a.N = d;
+            a.K = count;
+            a.live = z.live;
+            a.splits = p.dx.splits;
+            a.part = reinterpret_cast<float*>(base + p.dx_off);
+            a.part_stride = static_cast<size_t>(N) * d;
+            a.add = i > 0;
+            launch_product<true, false>(s, p.dx.narrow, a, N, st);
+        }
+        if (params) {
+            Product a{};
+            a.a = Operand{z.dz, 0, z.ldz};
+            a.b = Operand{v.x, 0, d};
+            a.M = count;
+            // (dbias alone: the product with x's first columns, whose tiles sum dz)
+            a.N = dweight != nullptr ? d : 8;
+            a.K = N;
+            a.live = z.live;
+            a.rows_are_k = 1;
+            a.splits = dweight != nullptr ? p.dw.splits : 1;
+            char* const dwp = dweight != nullptr ? static_cast<char*>(dweight) +
+                                                       static_cast<size_t>(first) * d * size
+                                                 : nullptr;
+            char* const dbp =
+                dbias != nullptr ? static_cast<char*>(dbias) + static_cast<size_t>(first) * size
+                                 : nullptr;
+            if (a.splits == 1) {
+                StoreArgs c{};
+                static_cast<Product&>(c) = a;
+                c.c = dwp;
+                c.sums = dbp;
+                c.bsum = static_cast<float*>(c.sums);
+                launch_product<false, false>(s, p.dw.narrow, c, count, st);
+            } else {
+                PartArgs c{};
+                static_cast<Product&>(c) = a;
+                c.part = reinterpret_cast<float*>(base + p.dw_off);
+                c.part_stride = static_cast<size_t>(count) * d;
+                c.part_sums =
+                    dbp != nullptr ? reinterpret_cast<float*>(base + p.sums_off) : nullptr;
+                c.bsum = c.part_sums;
+                launch_product<false, false>(s, p.dw.narrow, c, count, st);
+                const unsigned grid = cdiv(static_cast<long long>(count) * (d / 8), 256);
+                if (bf16)
+                    dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, a.splits,
+                                                    reinterpret_cast<uint16_t*>(dwp),
+                                                    reinterpret_cast<uint16_t*>(dbp), count, d);
+                else
+                    dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, a.splits,
+                                                    reinterpret_cast<float*>(dwp),
+                                                    reinterpret_cast<float*>(dbp), count, d);
+            }
+        }
+    }
+    if (dx != nullptr && N > 0) {
+        const unsigned grid = cdiv(static_cast<long long>(N) * (d / 8), 256);
+        const float* const part = reinterpret_cast<const float*>(base + p.dx_off);
+        const size_t stride = static_cast<size_t>(N) * d;
+        if (bf16)
+            dx_kernel<<<grid, 256, 0, st>>>(part, stride, p.dx.splits, v.place,
+                                            static_cast<uint16_t*>(dx), N, d);
+        else
+            dx_kernel<<<grid, 256, 0, st>>>(part, stride, p.dx.splits, v.place,
+                                            static_cast<float*>(dx), N, d);
+    }
+    return launch_status();
+}
+
+}  // namespace vmoe

@@ -1,0 +1,69 @@
+"""Python binding of the entry points of include/vmoe_head.h.
+
+A head over many classes with its losses: softmax cross entropy against labels and
+distillation from a teacher's top logits, with their gradients. Functions have the
+names and argument order of the C calls and take torch device tensors (or None for
+optional pointers); all arithmetic runs in libvmoe.so. Marshalling and the checks of
+tensors (type, layout, device, size: ValueError) run in the extension module _train;
+everything else is the library's status (VmoeError).
+"""
+from __future__ import annotations
+
+import ctypes
+import os
+
+from . import vmoe as V  # first: it loads libvmoe.so, which _train is linked to
+from . import _train
+from .vmoe import VMOE_BF16, VMOE_F32, VmoeError, _check, _lib  # noqa: F401
+
+HEADER = os.path.join(os.path.dirname(V.HEADER), "vmoe_head.h")
+
+VMOE_REDUCE_MEAN, VMOE_REDUCE_SUM = range(2)
+MAX_TEACHER = 256  # most entries of a teacher's list
+
+
+class HeadShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_rows", "d_model", "n_classes", "n_teacher", "dtype", "reduction")] + [
+        ("temperature", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+def _declare():
+    for name in ("saved", "fwd_workspace", "bwd_workspace"):
+        f = getattr(_lib, f"vmoe_head_loss_{name}_bytes")
+        f.restype, f.argtypes = ctypes.c_size_t, [ctypes.c_void_p]
+
+
+_declare()
+
+
+def make_head_shape(n_rows, d_model, n_classes, dtype, *, n_teacher=0, temperature=1.0,
+                    reduction=VMOE_REDUCE_MEAN) -> HeadShape:
+    """n_teacher: entries of the teacher's list, 0 without a teacher."""
+    return HeadShape(n_rows, d_model, n_classes, n_teacher, dtype, reduction, temperature, 0)
+
+
+def vmoe_head_loss_saved_bytes(shape: HeadShape) -> int:
+    return int(_lib.vmoe_head_loss_saved_bytes(ctypes.byref(shape)))
+
+
+def vmoe_head_loss_fwd_workspace_bytes(shape: HeadShape) -> int:
+    return int(_lib.vmoe_head_loss_fwd_workspace_bytes(ctypes.byref(shape)))
+
+
+def vmoe_head_loss_bwd_workspace_bytes(shape: HeadShape) -> int:
+    return int(_lib.vmoe_head_loss_bwd_workspace_bytes(ctypes.byref(shape)))
+
+
+def vmoe_head_loss_fwd(shape, x, weight, bias, labels, teacher_idx, teacher_logits, row_weight,
+                       losses, row_losses, saved, workspace, stream=None):
+    """saved: u8, vmoe_head_loss_saved_bytes of it, for vmoe_head_loss_bwd."""
+    _check("vmoe_head_loss_fwd", _train.head_loss_fwd(
+        shape, x, weight, bias, labels, teacher_idx, teacher_logits, row_weight, losses,
+        row_losses, saved, workspace, stream))
+
+
+def vmoe_head_loss_bwd(shape, weight, saved, w_label, w_teacher, dx, dweight, dbias, workspace,
+                       stream=None):
+    _check("vmoe_head_loss_bwd", _train.head_loss_bwd(
+        shape, weight, saved, w_label, w_teacher, dx, dweight, dbias, workspace, stream))
