@@ -20,7 +20,7 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
 
 namespace {
 
-constexpr int kMaxRows = 1 << 21, kMaxClasses = 1 << 24, kMaxWidth = 1 << 16;
+constexpr int kMaxRows = 1 << 21, kMaxClasses = 1 << 21, kMaxWidth = 1 << 16;
 constexpr long long kMaxTokens = 1LL << 30;   // N d: 32-bit byte offsets in bf16 rows
 constexpr long long kMaxLogits = 1LL << 36;   // N V: threads of one launch
 constexpr float kMaxTemperature = 1024.0f;

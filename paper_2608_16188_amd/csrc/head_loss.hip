@@ -8,13 +8,13 @@
 //             (1024 rows a block); the bias in f32, -infinity past the classes
 //   rows      a wave a row: the row's x to its place, its label and its teacher's
 //             entries with their q
-//   targets   the logits of those classes, by the same chain of matrix instructions
-//             as the tiles', so that they have the tiles' bits
-//   stats     z by tiles -> (max, sum of exponentials) of each row and strip
+//   sort      with a teacher, the entries by the tile of z that they lie in
+//   stats     z by tiles -> (max, sum of exponentials) of each row and strip, and the
+//             logits of labels and entries
 //   finish    lse of each row, its losses, their sums (last block, double)
 // and for each piece of the classes
-//   grad_z    z by tiles -> dz but for the targets, in the operands' type
-//   subtract  dz at the targets, in f32 from their logits, rounded once
+//   grad_z    z by tiles -> dz, in the operands' type
+//   subtract  with a teacher, dz at the targets, in f32 from their logits, rounded once
 //   product   dx += dz W (f32 partial sums in slots), dW = dz^T x, db = sums of dz
 // and in the end dx from the slots, rounded once, rows back to their places.
 // Only live rows reach the products: their number is read on the device, tiles past
@@ -47,6 +47,8 @@ size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 struct Header {
     int32_t live;      // rows with a label or a teacher
     int32_t labelled;  // labels were given
+    int32_t biased;    // a bias was
+    int32_t unused;
     float sum[2];      // of weights: rows with a label, with a teacher
 };
 
@@ -110,6 +112,10 @@ struct F32Tile {
 using TileBig = PhaseTile<4>;
 using TileNarrow = PhaseTile<3>;
 
+// Most tiles of classes (sort_kernel counts each in LDS).
+constexpr int kMaxClassTiles = 16384;
+static_assert((1 << 21) <= kMaxClassTiles * F32Tile::BN, "the largest number of classes");
+
 template <class T>
 constexpr bool is_f32() { return std::is_same<T, F32Tile>::value; }
 template <class T>
@@ -127,9 +133,13 @@ struct Product : GemmArgs {
 };
 
 struct StatsArgs : Product {
-    const float* zbias;  // [V up to 256]
+    const float* zbias;       // [V up to 256]
     float *mx, *sum, *sum_t;  // [strips][N]
-    int n_rows;
+    const int32_t* tidx;      // [N, per_row]: the rows' labels first
+    float* tz;                // and where their logits go, and the entries'
+    const uint32_t* list;     // entries by tile (sort_kernel), or null
+    const int32_t* ends;
+    int n_rows, per_row, has_bias;
     float scale, scale_t;     // log2 e / temperature of `sum` and of `sum_t`
     static constexpr int OUT = EPI_STORE;
 };
@@ -141,6 +151,8 @@ struct GradZArgs : Product {
     const float2* weight;
     void* dz;  // [N, ldz]
     int ldz;
+    const int32_t* label;  // [N] (without a teacher: with one, subtract_kernel sees to them)
+    int first;             // the piece's first class
     float w_label, w_teacher;  // w_teacher times T
     float inv_t;
     int mean, teacher;
@@ -404,22 +416,51 @@ __device__ __forceinline__ void add_bias(f32x16 (&acc)[T::FM][T::PB], const floa
         }
 }
 
+// Where a class lies in the wave's accumulators: 16 b + register, in the lane that
+// holds the class's column; -1 in the others and where it lies in another strip.
+template <class T>
+__device__ __forceinline__ int class_spot(int c, int n0) {
+    const int lane = threadIdx.x & 63, wn = wave_id() % T::WGN;
+    const int rel = c - n0 - 32 * wn;
+    const bool here = rel >= 0 && rel < 64 * T::PB && (rel & 32) == 0 &&
+                      ((rel >> 2) & 1) == (lane >> 5);
+    return here ? 16 * (rel >> 6) + 4 * ((rel & 31) >> 3) + (rel & 3) : -1;
+}
+
+// Between a wave's LDS writes and its reads of what other lanes wrote (LDS accesses of
+// one wave run in order: only the compiler is held).
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A 32 x 32 block of f32 accumulators into LDS: row r at s + 64 r (16-bit words), its
+// 16-byte chunk c at chunk c ^ (r mod 8).
+__device__ __forceinline__ void put_block(const f32x16& v, lds_u16* s) {
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<lds_v4*>(s + r * 64 + (((2 * q + h) ^ (r & 7)) << 3)) = __builtin_bit_cast(
+            v4i32, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
+}
+
+// LDS of a wave's own, 4 KB.
+__device__ __forceinline__ lds_u16* wave_lds(const LdsArrays& arrays) {
+    return (lds_u16*)(arrays.b6) + wave_id() * 2048;
+}
+
 // One 32 x 32 block of a wave's outputs to rows of `dst` (element type E), through LDS
 // of the wave's own: rows leave as 16-byte pieces, eight (f32) or four lanes a row.
 // Row r of the block goes to dst + r ld; rows from `rows` and columns from `cols`
-// (a multiple of 8 unless the row is padded beyond it) are left out. A wave's LDS
-// accesses run in order: no barrier.
+// (a multiple of 8 unless the row is padded beyond it) are left out; `flip` (bf16): a
+// mask over two rounded values, for their signs. A wave's LDS accesses run in order: no
+// barrier.
 template <typename E>
 __device__ __forceinline__ void store_block(const f32x16& v, lds_u16* s, E* dst, size_t ld,
-                                            int rows, int cols) {
+                                            int rows, int cols, uint32_t flip = 0) {
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     if constexpr (sizeof(E) == 4) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const v4i32 w = __builtin_bit_cast(
-                v4i32, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
-            *reinterpret_cast<lds_v4*>(s + r * 64 + (((2 * q + h) ^ (r & 7)) << 3)) = w;
-        }
+        put_block(v, s);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int rr = 8 * u + (lane >> 3), c = lane & 7;
@@ -432,8 +473,8 @@ __device__ __forceinline__ void store_block(const f32x16& v, lds_u16* s, E* dst,
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             *reinterpret_cast<lds_v2*>(s + r * 32 + ((q ^ ((r >> 2) & 3)) << 3) + 4 * h) =
-                v2i32{static_cast<int>(pack_bf16x2(v[4 * q], v[4 * q + 1])),
-                      static_cast<int>(pack_bf16x2(v[4 * q + 2], v[4 * q + 3]))};
+                v2i32{static_cast<int>(pack_bf16x2(v[4 * q], v[4 * q + 1]) ^ flip),
+                      static_cast<int>(pack_bf16x2(v[4 * q + 2], v[4 * q + 3]) ^ flip)};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int rr = 16 * u + (lane >> 2), c = lane & 3;
@@ -444,42 +485,42 @@ __device__ __forceinline__ void store_block(const f32x16& v, lds_u16* s, E* dst,
     }
 }
 
-// LDS of a wave's own, 4 KB.
-__device__ __forceinline__ lds_u16* wave_lds(const LdsArrays& arrays) {
-    return (lds_u16*)(arrays.b6) + wave_id() * 2048;
-}
-
-// Of each row and the wave's strip of columns: the largest z and the sum of
-// exp((z - that) / temperature).
+// Of each row and the wave's strip of columns: the largest z, m, and the sum of
+// 2^(z scale - m') with m' = m scale rounded to f32 (finish_kernel takes that rounding
+// out again: one fused operation an exponential, and still the largest term's p is
+// right to the last digit). Bound by the vector unit beside the matrix instructions: an
+// exponential is four slots, the rest 2.5.
 template <class T, int EPI>
 __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsArgs>& p,
                                             f32x16 (&acc)[T::FM][T::PB], float (&)[T::FM], bool,
-                                            const LdsArrays&, int, int M, int, int, int,
+                                            const LdsArrays& arrays, int, int M, int N, int, int,
                                             int fm_live) {
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int wm = wave / T::WGN, wn = wave % T::WGN;
-    add_bias<T>(acc, p.zbias, p.t_n0);
+    if (p.has_bias || N < T::BN) add_bias<T>(acc, p.zbias, p.t_n0);
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         if (i >= fm_live) break;
+        const int r0 = 64 * wm + 32 * i;
+        const size_t row = p.t_m0 + min(r0 + (lane & 31), M - 1);
+        const int spot = class_spot<T>(p.tidx[row * p.per_row], p.t_n0);
         float m = kLowest;
 #pragma unroll
         for (int b = 0; b < T::PB; ++b)
 #pragma unroll
             for (int c = 0; c < 16; ++c) m = fmaxf(m, acc[i][b][c]);
         m = fmaxf(m, __shfl_xor(m, 32, 64));
-        // (z - m first, exact where the two are near: with m scaled and rounded by itself
-        // the largest p would be off by its rounding)
         auto total = [&](float scale) {
+            const float at = m * scale;
             float s = 0.0f;
 #pragma unroll
             for (int b = 0; b < T::PB; ++b)
 #pragma unroll
                 for (int c = 0; c < 16; ++c)
-                    s += __builtin_amdgcn_exp2f((acc[i][b][c] - m) * scale);
+                    s += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][b][c], scale, -at));
             return s + __shfl_xor(s, 32, 64);
         };
-        const int r = 64 * wm + 32 * i + lane;  // (lanes below 32)
+        const int r = r0 + lane;  // (lanes below 32)
         const size_t at = static_cast<size_t>(p.t_n * T::WGN + wn) * p.n_rows + p.t_m0 + r;
         const float s = total(p.scale);
         const bool store = lane < 32 && r < M;
@@ -491,6 +532,41 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsA
             const float st = total(p.scale_t);
             if (store) p.sum_t[at] = st;
         }
+        if (__any(spot >= 0)) {  // (few strips hold a label)
+            float z = 0.0f;
+#pragma unroll
+            for (int b = 0; b < T::PB; ++b)
+#pragma unroll
+                for (int c = 0; c < 16; ++c) z = spot == 16 * b + c ? acc[i][b][c] : z;
+            if (spot >= 0 && r0 + (lane & 31) < M) p.tz[row * p.per_row] = z;
+        }
+    }
+    if (p.list == nullptr) return;
+    // The logits of the tile's entries: a lane an entry, 32 x 32 blocks with one of
+    // them through LDS.
+    const size_t tile = static_cast<size_t>(p.t_m0 / T::BM) * p.tiles_n + p.t_n;
+    const int to = p.ends[tile], from = p.t_n > 0 ? p.ends[tile - 1] : 0;
+    const uint32_t* const list = p.list + static_cast<size_t>(p.t_m0) * (p.per_row - 1);
+    lds_u16* const s = wave_lds(arrays);
+    for (int e0 = from; e0 < to; e0 += 64) {
+        const uint32_t e = e0 + lane < to ? list[e0 + lane] : 0;
+        const int r = e & 255, c = (e >> 8) & 255;
+        const bool mine = e0 + lane < to && (r >> 6) == wm && ((c >> 5) & 1) == wn;
+        const int block = mine ? ((r >> 5) & 1) * T::PB + (c >> 6) : -1;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+            for (int b = 0; b < T::PB; ++b) {
+                if (!__any(block == i * T::PB + b)) continue;
+                put_block(acc[i][b], s);
+                wave_lds_fence();
+                if (block == i * T::PB + b) {
+                    const int at = (r & 31) * 64 + ((((c >> 2) & 7) ^ (r & 7)) << 3) + 2 * (c & 3);
+                    p.tz[static_cast<size_t>(p.t_m0 + r) * p.per_row + 1 + (e >> 16)] =
+                        *reinterpret_cast<lds_f32*>(s + at);
+                }
+                wave_lds_fence();
+            }
     }
 }
 
@@ -521,18 +597,22 @@ struct Softmax {
     }
 };
 
-// dz without its targets. One softmax serves both losses where the temperature is 1 or
-// only one of them is there.
+// dz, but for a teacher's targets. One softmax serves both losses where the temperature
+// is 1 or only one of them is there. bf16: the weight goes into the exponent, a
+// row's sign into the rounded values, and lse into one constant, whose rounding moves
+// p by some 2^-24 |log2|, far below the rounding of dz; f32 keeps z - max z and the
+// logarithm of the sum apart.
 template <class T, int EPI>
 __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<GradZArgs>& p,
                                             f32x16 (&acc)[T::FM][T::PB], float (&)[T::FM], bool,
-                                            const LdsArrays& arrays, int, int M, int, int, int,
+                                            const LdsArrays& arrays, int, int M, int N, int, int,
                                             int fm_live) {
+    constexpr bool F32 = is_f32<T>();
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int wm = wave / T::WGN, wn = wave % T::WGN;
     const Header h = *p.head;
     const Softmax soft(h, p.teacher, p.inv_t);
-    add_bias<T>(acc, p.zbias, p.t_n0);
+    if (h.biased || N < T::BN) add_bias<T>(acc, p.zbias, p.t_n0);
     Elm<T>* const dz = static_cast<Elm<T>*>(p.dz);
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
@@ -540,19 +620,49 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<GradZA
         const int r0 = 64 * wm + 32 * i, r = p.t_m0 + min(r0 + (lane & 31), M - 1);
         const float4 rec = p.rec[r];
         const float2 g = row_rates(h, p.weight[r], p.w_label, p.w_teacher, p.mean);
+        const int spot = p.label != nullptr ? class_spot<T>(p.label[r] - p.first, p.t_n0) : -1;
+        const bool any = __any(spot >= 0);
+        const float all = g.x + g.y;
+        const bool down = !F32 && !soft.two && all < 0.0f;
+        const float hit = down ? -g.x : g.x;
+        // -(lse - log2 |weight|)
+        const float c1 = __builtin_fmaf(rec.x, -soft.scale, -rec.y) +
+                         log2f(fabsf(soft.two ? g.x : all));
+        const float c2 = __builtin_fmaf(rec.x, -soft.scale_t, -rec.z) + log2f(fabsf(g.y));
+        const float s1 = copysignf(1.0f, g.x), s2 = copysignf(1.0f, g.y);
 #pragma unroll
         for (int b = 0; b < T::PB; ++b) {
             f32x16 v;
             if (soft.two) {
 #pragma unroll
-                for (int c = 0; c < 16; ++c) v[c] = soft.at<true>(acc[i][b][c], rec, g);
+                for (int c = 0; c < 16; ++c) {
+                    const float z = acc[i][b][c];
+                    if constexpr (F32) {
+                        v[c] = soft.at<true>(z, rec, g);
+                    } else {
+                        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z, soft.scale, c1));
+                        const float e2 =
+                            __builtin_amdgcn_exp2f(__builtin_fmaf(z, soft.scale_t, c2));
+                        v[c] = __builtin_fmaf(e1, s1, e2 * s2);
+                    }
+                }
             } else {
 #pragma unroll
-                for (int c = 0; c < 16; ++c) v[c] = soft.at<false>(acc[i][b][c], rec, g);
+                for (int c = 0; c < 16; ++c) {
+                    const float z = acc[i][b][c];
+                    if constexpr (F32) v[c] = soft.at<false>(z, rec, g);
+                    else v[c] = __builtin_amdgcn_exp2f(__builtin_fmaf(z, soft.scale, c1));
+                }
+            }
+            if (any) {  // (p - 1 from z - max z, before any rounding)
+#pragma unroll
+                for (int c = 0; c < 16; ++c)
+                    if (spot == 16 * b + c)
+                        v[c] = (down ? -1.0f : 1.0f) * soft.at<false>(acc[i][b][c], rec, g) - hit;
             }
             const int n = p.t_n0 + 64 * b + 32 * wn;
             store_block(v, wave_lds(arrays), dz + static_cast<size_t>(p.t_m0 + r0) * p.ldz + n,
-                        p.ldz, M - r0, p.ldz - n);
+                        p.ldz, M - r0, p.ldz - n, down ? 0x80008000u : 0u);
         }
     }
 }
@@ -668,13 +778,44 @@ __global__ __launch_bounds__(kMarkRows) void mark_kernel(MarkArgs p) {
     }
     __shared__ int wsum[kMarkRows / 64];
     const int t = blockIdx.x * kMarkRows + tid;
-    bool live = false;
-    if (t < p.N && (p.row_weight == nullptr || p.row_weight[t] != 0.0f)) {
-        live = p.labels != nullptr && is_class(p.labels[t], p.V);
+    const bool counts = t < p.N && (p.row_weight == nullptr || p.row_weight[t] != 0.0f);
+    bool live = counts && p.labels != nullptr && is_class(p.labels[t], p.V);
+    // rows without a label: whether their list has an entry. Mostly the first is one;
+    // the other rows eight at a time by the whole wave, classes before logits (lists
+    // of padding have neither)
+    if (counts && !live && p.K > 0) {
         const size_t at = static_cast<size_t>(t) * p.K;
-        for (int j = 0; j < p.K && !live; ++j)
-            live = is_class(p.teacher_idx[at + j], p.V) &&
-                   p.teacher_logits[at + j] != -__builtin_inff();
+        live = is_class(p.teacher_idx[at], p.V) && p.teacher_logits[at] != -__builtin_inff();
+    }
+    uint64_t open = p.K > 1 ? __ballot(counts && !live) : 0;
+    while (open != 0) {
+        constexpr int U = 8;
+        int row[U];
+        uint64_t found[U];
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+            row[v] = open != 0 ? __ffsll(static_cast<long long>(open)) - 1 : row[0];
+            found[v] = 0;
+            open &= open - 1;
+        }
+        for (int j0 = 0; j0 < p.K; j0 += 64) {
+            const int j = j0 + lane;
+            bool there[U];
+#pragma unroll
+            for (int v = 0; v < U; ++v)
+                there[v] = j < p.K &&
+                           is_class(p.teacher_idx[static_cast<size_t>(t - lane + row[v]) * p.K + j],
+                                    p.V);
+#pragma unroll
+            for (int v = 0; v < U; ++v)
+                if (there[v])
+                    there[v] = p.teacher_logits[static_cast<size_t>(t - lane + row[v]) * p.K + j] !=
+                               -__builtin_inff();
+#pragma unroll
+            for (int v = 0; v < U; ++v) found[v] |= __ballot(there[v]);
+        }
+#pragma unroll
+        for (int v = 0; v < U; ++v) live |= lane == row[v] && found[v] != 0;
     }
     const uint64_t all = __ballot(live);
     if (lane == 0) wsum[wave] = __popcll(all);
@@ -693,13 +834,6 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return v;
-}
-
-// Between a wave's LDS writes and its reads of what other lanes wrote (LDS accesses of
-// one wave run in order: only the compiler is held).
-__device__ __forceinline__ void wave_lds_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
 }
 
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
@@ -726,7 +860,7 @@ struct RowArgs {
     const float* row_weight;
     const int32_t* counts;
     Saved s;
-    int N, V, K, d, row_blocks;
+    int N, V, K, d, row_blocks, biased;
     float inv_t;
 };
 
@@ -748,6 +882,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
         if (lane == 0) {
             p.s.head->live = all;
             p.s.head->labelled = p.labels != nullptr;
+            p.s.head->biased = p.biased;
         }
     }
     if (t >= p.N) return;
@@ -824,86 +959,67 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
     }
 }
 
-struct TargetArgs {
+struct SortArgs {
     Saved s;
-    const void* weight;
-    int K, d;
+    uint32_t* list;  // [N, K]: row | class << 8 | entry << 16, row and class in the tile
+    int32_t* ends;   // [row tiles][class tiles]: where a tile's entries end in its rows' list
+    int K, tile_rows, tile_shift, tiles_n;
 };
 
-// Logits of the rows' targets, 32 pairs of a row and a class a wave: the diagonal of
-// the pairs' 32 x 32 product. The other products are thrown away, but the sums have
-// the bits of the tiles' (the same instructions on the same k, in order), which p - 1
-// and p - q need where they are small: a sum in another order, off by 1e-6 at logits
-// of 14, left 1 - p of a row that is nearly certain with three digits.
-template <typename E>
-__global__ __launch_bounds__(256) void targets_kernel(TargetArgs p) {
-    const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
-    const long long first = 32LL * (4LL * blockIdx.x + wave);
-    const int n = 1 + p.K;
-    const long long pairs = static_cast<long long>(p.s.head->live) * n;
-    if (first >= pairs) return;
-    const long long pair = first + (lane & 31);
-    const bool in = pair < pairs;
-    const int c = in ? p.s.tidx[pair] : -1;
-    if (!__any(c >= 0)) {
-        if (in && h == 0) p.s.tz[pair] = 0.0f;
-        return;
-    }
-    const E* const w = static_cast<const E*>(p.weight) + static_cast<size_t>(max(c, 0)) * p.d;
-    const E* const x = static_cast<const E*>(p.s.x) + static_cast<size_t>(in ? pair / n : 0) * p.d;
-    f32x16 acc;
-#pragma unroll
-    for (int q = 0; q < 16; ++q) acc[q] = 0.0f;
-    if constexpr (sizeof(E) == 2) {
-        constexpr int U = 8;  // steps of 16 k in flight
-        for (int k0 = 0; k0 < p.d; k0 += 16 * U) {
-            uint4 fw[U], fx[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int k = k0 + 16 * u + 8 * h;
-                fw[u] = fx[u] = make_uint4(0u, 0u, 0u, 0u);
-                if (k < p.d) {
-                    fw[u] = *reinterpret_cast<const uint4*>(w + k);
-                    fx[u] = *reinterpret_cast<const uint4*>(x + k);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    __builtin_bit_cast(bf16x8, fw[u]), __builtin_bit_cast(bf16x8, fx[u]), acc, 0, 0,
-                    0);
+// The entries of a tile's rows by class tile, a block: counts in LDS, their sums, then
+// every entry to its tile's next place (in any order: each has a logit of its own).
+__global__ __launch_bounds__(1024) void sort_kernel(SortArgs p) {
+    __shared__ int at_s[kMaxClassTiles];
+    __shared__ int wave_s[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int r0 = blockIdx.x * p.tile_rows;
+    const int rows = min(p.tile_rows, p.s.head->live - r0);
+    if (rows <= 0) return;
+    const int entries = rows * p.K;
+    const size_t first = static_cast<size_t>(r0) * (1 + p.K);
+    for (int t = tid; t < p.tiles_n; t += 1024) at_s[t] = 0;
+    __syncthreads();
+    auto each = [&](auto f) {
+#pragma unroll 4
+        for (int e = tid; e < entries; e += 1024) {
+            const int r = e / p.K, j = e - r * p.K;
+            f(r, j, first + static_cast<size_t>(r) * (1 + p.K) + 1 + j);
         }
-    } else {
-        constexpr int U = 8;  // steps of 8 k in flight
-        for (int k0 = 0; k0 < p.d; k0 += 8 * U) {
-            float4 fw[U], fx[U];
+    };
+    each([&](int, int, size_t at) {
+        const int c = p.s.tidx[at];
+        if (c >= 0) atomicAdd(&at_s[c >> p.tile_shift], 1);
+        else p.s.tz[at] = 0.0f;
+    });
+    __syncthreads();
+    // exclusive sums: runs of `per` tiles a thread
+    const int per = (p.tiles_n + 1023) / 1024, t0 = tid * per, t1 = min(t0 + per, p.tiles_n);
+    int sum = 0;
+    for (int t = t0; t < t1; ++t) sum += at_s[t];
+    int before = sum;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int k = k0 + 8 * u + 4 * h;
-                fw[u] = fx[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (k < p.d) {
-                    fw[u] = *reinterpret_cast<const float4*>(w + k);
-                    fx[u] = *reinterpret_cast<const float4*>(x + k);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fw[u].x, fx[u].x, acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fw[u].y, fx[u].y, acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fw[u].z, fx[u].z, acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fw[u].w, fx[u].w, acc, 0, 0, 0);
-            }
-        }
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(before, o, 64);
+        if (lane >= o) before += v;
     }
-    // register 4 q + r of lane l: class 8 q + 4 (l / 32) + r against row l % 32
-    const int j = lane & 31;
-    float z = 0.0f;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (8 * q + 4 * h + r == j) z = acc[4 * q + r];
-    if (((j >> 2) & 1) == h && in) p.s.tz[pair] = c >= 0 ? z + p.s.bias[c] : 0.0f;
+    if (lane == 63) wave_s[wave] = before;
+    __syncthreads();
+    before -= sum;
+    for (int w = 0; w < wave; ++w) before += wave_s[w];
+    for (int t = t0; t < t1; ++t) {
+        const int n = at_s[t];
+        at_s[t] = before;
+        before += n;
+        p.ends[static_cast<size_t>(blockIdx.x) * p.tiles_n + t] = before;
+    }
+    __syncthreads();
+    uint32_t* const list = p.list + static_cast<size_t>(r0) * p.K;
+    each([&](int r, int j, size_t at) {
+        const int c = p.s.tidx[at];
+        if (c < 0) return;
+        const int o = atomicAdd(&at_s[c >> p.tile_shift], 1);
+        list[o] = static_cast<uint32_t>(r | (c & ((1 << p.tile_shift) - 1)) << 8 | j << 16);
+    });
 }
 
 struct FinishArgs {
@@ -916,41 +1032,71 @@ struct FinishArgs {
     float temperature, inv, inv_t;  // inv: of `sum`'s softmax
 };
 
-constexpr int kFinishWaves = 8;
+constexpr int kFinishWaves = 16;
 
-// 64 live rows a block, a lane each; the waves share the strips.
+// What a row has of z so far: the largest, and the sums of exp of z less that, over
+// either temperature.
+struct RowSums {
+    float m = kLowest, s = 0.0f, t = 0.0f;
+    // U strips (or waves) more; raw: their sums are about a rounded maximum (StatsArgs)
+    template <int U, bool RAW>
+    __device__ __forceinline__ void join(const float (&m2)[U], const float (&s2)[U],
+                                         const float (&t2)[U], float scale, float scale_t,
+                                         bool two) {
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = fmaxf(top, m2[u]);
+        auto part = [&](float mu, float sc, bool raw) {
+            float x = (mu - top) * sc;
+            if (raw) x -= __builtin_fmaf(mu, sc, -(mu * sc));
+            return __builtin_amdgcn_exp2f(x);
+        };
+        s *= part(m, scale, false);
+        if (two) t *= part(m, scale_t, false);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            s += s2[u] * part(m2[u], scale, RAW);
+            if (two) t += t2[u] * part(m2[u], scale_t, RAW);
+        }
+        m = top;
+    }
+};
+
+// 64 live rows a block, a lane each; the waves share the strips, four at a time.
 __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p) {
     // max z / T and z / T of a target are to be rounded alike: their difference counts
 #pragma clang fp contract(off)
-    constexpr int W = kFinishWaves;
+    constexpr int W = kFinishWaves, U = 4;
     __shared__ float mx_s[W][64], sum_s[W][64], sumt_s[W][64], cross_s[W][64];
     __shared__ double part_s[W][4];
     __shared__ bool last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int live = p.s.head->live;
     const int r = blockIdx.x * 64 + lane;
-    const bool in = r < live;
-    auto join = [&](float& m, float& s, float& st, float m2, float s2, float st2) {
-        const float top = fmaxf(m, m2);
-        const float scale = kLog2e * p.inv, scale_t = kLog2e * p.inv_t;
-        const float a = (m - top) * scale, b = (m2 - top) * scale;
-        s = s * __builtin_amdgcn_exp2f(a) + s2 * __builtin_amdgcn_exp2f(b);
-        if (p.sum_t != nullptr) {
-            const float at = (m - top) * scale_t, bt = (m2 - top) * scale_t;
-            st = st * __builtin_amdgcn_exp2f(at) + st2 * __builtin_amdgcn_exp2f(bt);
-        }
-        m = top;
-    };
-    float m = kLowest, s = 0.0f, st = 0.0f, cross = 0.0f;
+    const bool in = r < live, two = p.sum_t != nullptr;
+    const float scale = kLog2e * p.inv, scale_t = kLog2e * p.inv_t;
+    RowSums z;
+    float cross = 0.0f;
     if (in) {
         const size_t entry = static_cast<size_t>(r) * (1 + p.K);
+#pragma unroll 4
         for (int j = 1 + wave; j <= p.K; j += W)  // (z of an entry that is none is 0)
             cross = __builtin_fmaf(p.s.tq[entry + j], p.s.tz[entry + j] * p.inv_t, cross);
-        for (int q = wave; q < p.strips; q += W) {
-            const size_t at = static_cast<size_t>(q) * p.N + r;
-            join(m, s, st, p.mx[at], p.sum[at], p.sum_t != nullptr ? p.sum_t[at] : 0.0f);
+        for (int q = wave; q < p.strips; q += U * W) {
+            float m2[U], s2[U], t2[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool there = q + u * W < p.strips;
+                const size_t at = static_cast<size_t>(there ? q + u * W : q) * p.N + r;
+                m2[u] = p.mx[at];
+                s2[u] = p.sum[at];
+                t2[u] = two ? p.sum_t[at] : 0.0f;
+                if (!there) s2[u] = t2[u] = 0.0f;
+            }
+            z.join<U, true>(m2, s2, t2, scale, scale_t, two);
         }
     }
+    float m = z.m, s = z.s, st = z.t;
     mx_s[wave][lane] = m;
     sum_s[wave][lane] = s;
     sumt_s[wave][lane] = st;
@@ -959,11 +1105,18 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     if (wave == 0) {
         double v[4] = {0.0, 0.0, 0.0, 0.0};
         if (in) {
+            float m2[W - 1], s2[W - 1], t2[W - 1];
 #pragma unroll
             for (int w = 1; w < W; ++w) {
-                join(m, s, st, mx_s[w][lane], sum_s[w][lane], sumt_s[w][lane]);
+                m2[w - 1] = mx_s[w][lane];
+                s2[w - 1] = sum_s[w][lane];
+                t2[w - 1] = sumt_s[w][lane];
                 cross += cross_s[w][lane];
             }
+            z.join<W - 1, false>(m2, s2, t2, scale, scale_t, two);
+            m = z.m;
+            s = z.s;
+            st = z.t;
             if (p.sum_t == nullptr) st = s;
             const float2 weight = p.s.weight[r];
             float4 rec = p.s.rec[r];
@@ -1037,34 +1190,48 @@ struct SubtractArgs {
     float w_label, w_teacher, inv_t;
 };
 
-// dz at a row's targets: a wave a row, a lane an entry. Entries of one class (a label
-// among the teacher's) write the same value, which each of them sums in the same order.
-template <typename E>
+// dz at a row's label and its teacher's entries: a wave a row, R entries a lane. Entries
+// of one class (the label is mostly among the teacher's) write the same value, which
+// each of them sums in the same order.
+template <typename E, int R>
 __global__ __launch_bounds__(256) void subtract_kernel(SubtractArgs p) {
-    __shared__ int idx_s[4][VMOE_HEAD_MAX_TEACHER + 1];
-    __shared__ float q_s[4][VMOE_HEAD_MAX_TEACHER + 1];
-    const int lane = threadIdx.x & 63, wave = wave_id(), r = blockIdx.x * 4 + wave;
+    const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + wave_id();
     const Header h = *p.s.head;
     if (r >= h.live) return;
     const int n = 1 + p.K;
     const size_t at = static_cast<size_t>(r) * n;
     const float4 rec = p.s.rec[r];
     const float2 g = row_rates(h, p.s.weight[r], p.w_label, p.w_teacher, p.mean);
-    for (int e = lane; e < n; e += 64) {
-        idx_s[wave][e] = p.s.tidx[at + e];
-        q_s[wave][e] = e == 0 ? g.x : g.y * p.s.tq[at + e];
-    }
-    wave_lds_fence();
     const Softmax soft(h, p.teacher, p.inv_t);
+    int idx[R];
+    float share[R], z[R], hit[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int e = lane + 64 * i;
+        idx[i] = e < n ? p.s.tidx[at + e] : -1;
+        share[i] = e < n ? (e == 0 ? g.x : g.y * p.s.tq[at + e]) : 0.0f;
+        z[i] = e < n ? p.s.tz[at + e] : 0.0f;
+        hit[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int most = min(64, n - 64 * i);
+#pragma unroll 4
+        for (int o = 0; o < most; ++o) {
+            const int c = __builtin_amdgcn_readlane(idx[i], o);
+            const float v = __builtin_bit_cast(
+                float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, share[i]), o));
+#pragma unroll
+            for (int k = 0; k < R; ++k) hit[k] += idx[k] == c ? v : 0.0f;
+        }
+    }
     E* const dz = static_cast<E*>(p.dz) + static_cast<size_t>(r) * p.ldz;
-    for (int e = lane; e < n; e += 64) {
-        const int c = idx_s[wave][e];
-        if (c < p.first || c >= p.first + p.count) continue;
-        const float z = p.s.tz[at + e];
-        const float v = soft.two ? soft.at<true>(z, rec, g) : soft.at<false>(z, rec, g);
-        float hit = 0.0f;
-        for (int o = 0; o < n; ++o) hit += idx_s[wave][o] == c ? q_s[wave][o] : 0.0f;
-        Elem<E>::store(dz, c - p.first, v - hit);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int c = idx[i] - p.first;
+        if (idx[i] < 0 || c < 0 || c >= p.count) continue;
+        const float v = soft.two ? soft.at<true>(z[i], rec, g) : soft.at<false>(z[i], rec, g);
+        Elem<E>::store(dz, c, v - hit[i]);
     }
 }
 
@@ -1081,6 +1248,7 @@ __global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ part,
     float v[8] = {};
     if (r >= 0) {
         const float* at = part + static_cast<size_t>(r) * d + c;
+#pragma unroll 8
         for (int s = 0; s < slots; ++s) {
             float w[8];
             load8(at + s * stride, w);
@@ -1114,6 +1282,7 @@ __global__ __launch_bounds__(256) void dw_kernel(const float* __restrict__ part,
     }
     if (i >= static_cast<long long>(M) * per) return;
     float v[8] = {};
+#pragma unroll 4
     for (int s = 0; s < slots; ++s) {
         float w[8];
         load8(part + s * stride + 8 * i, w);
@@ -1217,21 +1386,23 @@ Plan make_plan(const vmoe_head_shape& s) {
     return p;
 }
 
-template <class T>
-int strips_of(const vmoe_head_shape& s) {
-    return static_cast<int>(cdiv(s.n_classes, T::BN)) * T::WGN;
-}
+static_assert(TileBig::BN == 256 && TileBig::WGN == 2 && F32Tile::BN == 128 && F32Tile::WGN == 2,
+              "two strips a tile of z");
 
 struct FwdPlan {
     int row_blocks, strips, finish_blocks, two;
-    size_t counts_off, ticket_off, sums_off, mx_off, sum_off, sumt_off, bytes;
+    int tile_rows, tile_shift, tiles_n;  // of z
+    size_t counts_off, ticket_off, sums_off, mx_off, sum_off, sumt_off, list_off, ends_off, bytes;
 };
 
 FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     FwdPlan p;
     const size_t N = s.n_rows;
     p.row_blocks = static_cast<int>(cdiv(s.n_rows, kMarkRows));
-    p.strips = s.dtype == VMOE_BF16 ? strips_of<TileBig>(s) : strips_of<F32Tile>(s);
+    p.tile_rows = s.dtype == VMOE_BF16 ? TileBig::BM : F32Tile::BM;
+    p.tile_shift = s.dtype == VMOE_BF16 ? 8 : 7;
+    p.tiles_n = static_cast<int>(cdiv(s.n_classes, 1 << p.tile_shift));
+    p.strips = 2 * p.tiles_n;
     p.finish_blocks = s.n_rows > 0 ? static_cast<int>(cdiv(s.n_rows, 64)) : 1;
     p.two = labels && s.n_teacher > 0 && s.temperature != 1.0f;
     Carver c{nullptr};
@@ -1246,6 +1417,10 @@ FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     p.mx_off = take(4 * N * p.strips);
     p.sum_off = take(4 * N * p.strips);
     p.sumt_off = take(p.two ? 4 * N * p.strips : 0);
+    p.list_off = take(4 * N * s.n_teacher);
+    p.ends_off = take(s.n_teacher > 0 ? 4 * cdiv(s.n_rows, p.tile_rows) *
+                                            static_cast<size_t>(p.tiles_n)
+                                      : 0);
     p.bytes = c.off;
     return p;
 }
@@ -1293,17 +1468,14 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
     mark_kernel<<<p.row_blocks + cdiv(padded_classes(s), kMarkRows), kMarkRows, 0, st>>>(m);
     const float inv_t = 1.0f / s.temperature;
     const RowArgs t{x, labels, teacher_idx, teacher_logits, row_weight, m.counts, v,
-                    N, V, K, s.d_model, p.row_blocks, inv_t};
+                    N, V, K, s.d_model, p.row_blocks, bias != nullptr, inv_t};
     const unsigned row_grid = N > 0 ? cdiv(N, 4) : 1;
-    const TargetArgs g{v, weight, K, s.d_model};
-    const unsigned pair_grid = cdiv(static_cast<long long>(N) * (1 + K), 128);
-    if (s.dtype == VMOE_BF16) {
-        rows_kernel<uint16_t><<<row_grid, 256, 0, st>>>(t);
-        if (N > 0) targets_kernel<uint16_t><<<pair_grid, 256, 0, st>>>(g);
-    } else {
-        rows_kernel<float><<<row_grid, 256, 0, st>>>(t);
-        if (N > 0) targets_kernel<float><<<pair_grid, 256, 0, st>>>(g);
-    }
+    if (s.dtype == VMOE_BF16) rows_kernel<uint16_t><<<row_grid, 256, 0, st>>>(t);
+    else rows_kernel<float><<<row_grid, 256, 0, st>>>(t);
+    const SortArgs g{v, reinterpret_cast<uint32_t*>(base + p.list_off),
+                     reinterpret_cast<int32_t*>(base + p.ends_off), K, p.tile_rows, p.tile_shift,
+                     p.tiles_n};
+    if (N > 0 && K > 0) sort_kernel<<<cdiv(N, p.tile_rows), 1024, 0, st>>>(g);
 
     StatsArgs a{};
     a.a = Operand{v.x, 0, s.d_model};
@@ -1317,7 +1489,13 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
     a.mx = reinterpret_cast<float*>(base + p.mx_off);
     a.sum = reinterpret_cast<float*>(base + p.sum_off);
     a.sum_t = p.two ? reinterpret_cast<float*>(base + p.sumt_off) : nullptr;
+    a.tidx = v.tidx;
+    a.tz = v.tz;
+    a.list = K > 0 ? g.list : nullptr;
+    a.ends = g.ends;
     a.n_rows = N;
+    a.per_row = 1 + K;
+    a.has_bias = bias != nullptr;
     a.scale_t = kLog2e * inv_t;
     a.scale = K > 0 && labels == nullptr ? a.scale_t : kLog2e;
     launch_product<true, true>(s, 0, a, N, st);
@@ -1364,12 +1542,19 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
         z.inv_t = 1.0f / s.temperature;
         z.mean = s.reduction == VMOE_REDUCE_MEAN;
         z.teacher = s.n_teacher > 0;
+        z.label = z.teacher ? nullptr : v.tidx;
+        z.first = first;
         launch_product<true, true>(s, 0, z, N, st);
-        if (N > 0) {
+        if (N > 0 && z.teacher) {
             const SubtractArgs u{v, z.dz, z.ldz, first, count, s.n_teacher, z.mean, z.teacher,
                                  z.w_label, z.w_teacher, z.inv_t};
-            if (bf16) subtract_kernel<uint16_t><<<cdiv(N, 4), 256, 0, st>>>(u);
-            else subtract_kernel<float><<<cdiv(N, 4), 256, 0, st>>>(u);
+            auto go = [&](auto entries) {
+                constexpr int R = decltype(entries)::value;
+                if (bf16) subtract_kernel<uint16_t, R><<<cdiv(N, 4), 256, 0, st>>>(u);
+                else subtract_kernel<float, R><<<cdiv(N, 4), 256, 0, st>>>(u);
+            };
+            if (s.n_teacher < 64) go(std::integral_constant<int, 1>{});
+            else go(std::integral_constant<int, (VMOE_HEAD_MAX_TEACHER + 64) / 64>{});
         }
         if (dx != nullptr) {
             PartArgs a{};
