@@ -15,7 +15,7 @@
 // and for each piece of the classes
 //   grad_z    z by tiles -> dz, in the operands' type
 //   subtract  with a teacher, dz at the targets, in f32 from their logits, rounded once
-//   product   dx += dz W (f32 partial sums in slots), dW = dz^T x, db = sums of dz
+//   products  dx += dz W (f32 partial sums in slots), dW = dz^T x, db = sums of dz
 // and in the end dx from the slots, rounded once, rows back to their places.
 // Only live rows reach the products: their number is read on the device, tiles past
 // it end at once, so padding costs nothing and the host waits for nothing.
@@ -107,7 +107,10 @@ Saved saved_layout(const vmoe_head_shape& s, void* base) {
 // columns lie in the tile as in the phased bf16 tiles (64 wm + 32 i, 64 b + 32 wn).
 struct F32Tile {
     static constexpr int PB = 2, BM = 128, BN = 128, WGN = 2, NT = 256, FM = 2, WM = 64;
+    static constexpr int WAVES_PER_EU = 4;
     static constexpr int KB = 16, OP_EL = BM * KB;
+    // LDS: two stages of both operands, in S_EL (16-bit words)
+    static constexpr int A_EL = 1, BL_EL = 1, BH_EL = 1, S_EL = 4 * OP_EL * 2;
 };
 using TileBig = PhaseTile<4>;
 using TileNarrow = PhaseTile<3>;
@@ -142,6 +145,7 @@ struct StatsArgs : Product {
     int n_rows, per_row, has_bias;
     float scale, scale_t;     // log2 e / temperature of `sum` and of `sum_t`
     static constexpr int OUT = EPI_STORE;
+    static constexpr bool A_KMAJOR = true, B_KMAJOR = true;
 };
 
 struct GradZArgs : Product {
@@ -157,20 +161,25 @@ struct GradZArgs : Product {
     float inv_t;
     int mean, teacher;
     static constexpr int OUT = EPI_STORE;
+    static constexpr bool A_KMAJOR = true, B_KMAJOR = true;
 };
 
-struct PartArgs : Product {  // f32 sums of each range of k
+// f32 sums of each range of k. LEFT: dz times the weight, else dz^T times x.
+template <bool LEFT>
+struct PartArgs : Product {
     float* part;       // [splits][M, N]
     size_t part_stride;
     float* part_sums;  // [splits][M] of A's rows, or null
     int add;           // to what is there
     static constexpr int OUT = EPI_F32;
+    static constexpr bool A_KMAJOR = LEFT, B_KMAJOR = false;
 };
 
-struct StoreArgs : Product {  // rounded, k in one range
+struct StoreArgs : Product {  // dz^T times x, rounded, k in one range
     void* c;      // [M, N], or null
     void* sums;   // [M] of A's rows, or null
     static constexpr int OUT = EPI_F32;
+    static constexpr bool A_KMAJOR = false, B_KMAJOR = false;
 };
 
 // The tile that finish_tile is called for.
@@ -183,9 +192,10 @@ struct Tiled : ARGS {
 // tiles go in groups of group_m rows of tiles, so that an XCD's blocks share operand
 // panels in its L2.
 template <int BM, class ARGS>
-__device__ __forceinline__ bool take_tile(const ARGS& p, int M, int* tm, int* tn, int* split) {
-    const int l = blockIdx.x >> 3;
-    int w = ((l / p.chunk) * 8 + (blockIdx.x & 7)) * p.chunk + l % p.chunk;
+__device__ __forceinline__ bool take_tile(const ARGS& p, int block, int M, int* tm, int* tn,
+                                          int* split) {
+    const int l = block >> 3;
+    int w = ((l / p.chunk) * 8 + (block & 7)) * p.chunk + l % p.chunk;
     const int tiles_m = (M + BM - 1) / BM, tiles = tiles_m * p.tiles_n;
     if (w >= tiles * p.splits) return false;
     *split = w / tiles;
@@ -202,20 +212,22 @@ __device__ __forceinline__ uint32_t record_bytes(long long bytes) {
     return static_cast<uint32_t>(bytes < 0x7FFFFFF0LL ? bytes : 0x7FFFFFF0LL);
 }
 
-template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
+template <class T, class ARGS>
 __device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const float* b, int M,
                                          int N, int K, float* lds);
 
 // One tile: the operands are taken from the tile's corner and its range of k on, so that
 // offsets inside it fit 32 bits however large they are.
-template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
-__device__ __forceinline__ bool place_tile(const ARGS& args, Tiled<ARGS>* p, const Elm<T>** a,
-                                           const Elm<T>** b, int* M, int* N, int* K) {
+template <class T, class ARGS>
+__device__ __forceinline__ bool place_tile(const ARGS& args, int block, Tiled<ARGS>* p,
+                                           const Elm<T>** a, const Elm<T>** b, int* M, int* N,
+                                           int* K) {
+    constexpr bool A_KMAJOR = ARGS::A_KMAJOR, B_KMAJOR = ARGS::B_KMAJOR;
     const int live = *args.live;
     const int rows = args.rows_are_k ? args.M : min(live, args.M);
     const int depth = args.rows_are_k ? min(live, args.K) : args.K;
     int tm, tn, split;
-    if (!take_tile<T::BM>(args, rows, &tm, &tn, &split)) return false;
+    if (!take_tile<T::BM>(args, block, rows, &tm, &tn, &split)) return false;
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
     split = __builtin_amdgcn_readfirstlane(split);
@@ -238,10 +250,36 @@ __device__ __forceinline__ bool place_tile(const ARGS& args, Tiled<ARGS>* p, con
     return true;
 }
 
-template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
+template <class T, class ARGS>
+__device__ __forceinline__ void run_tile(const ARGS& args, int block, uint16_t* a0, uint16_t* a1,
+                                         uint16_t* bl0, uint16_t* bh0, uint16_t* bl1,
+                                         uint16_t* bh1, uint16_t* stg) {
+    Tiled<ARGS> p;
+    const Elm<T>*a, *b;
+    int M, N, K;
+    if (!place_tile<T>(args, block, &p, &a, &b, &M, &N, &K)) return;
+    if constexpr (is_f32<T>()) {
+        f32_tile<T>(p, a, b, M, N, K, reinterpret_cast<float*>(stg));
+    } else {
+        constexpr bool AK = ARGS::A_KMAJOR, BK = ARGS::B_KMAJOR;
+        // bytes from the corner on: of a tile's rows, or of a range's k rows
+        const long long lda = args.a.ld, ldb = args.b.ld;
+        const auto ra = make_rsrc(a, record_bytes(2 * (AK ? min(M, T::BM) * lda : K * lda)));
+        const auto rb = make_rsrc(b, record_bytes(2 * (BK ? min(N, T::BN) * ldb : K * ldb)));
+        phase_tile<T, AK, BK, ARGS::OUT, 0>(p, ra, rb, 0, M, N, K, 0, 0, p.t_n, a0, a1, bl0, bh0,
+                                            bl1, bh1, stg);
+    }
+}
+
+struct NoProduct {};
+
+// A tile a block: the first product's on `blocks` blocks (a multiple of 8, so that the
+// XCDs stay as they are), the second's behind them, where they fill the CUs that the
+// first's last tiles leave.
+template <class T, class FIRST, class SECOND>
 __global__ __launch_bounds__(T::NT)
-__attribute__((amdgpu_waves_per_eu(2, 2)))
-void product_bf16_kernel(ARGS args) {
+__attribute__((amdgpu_waves_per_eu(T::WAVES_PER_EU, T::WAVES_PER_EU)))
+void product_kernel(FIRST first, SECOND second, int blocks) {
     __shared__ __attribute__((aligned(1024))) uint16_t a0[T::A_EL];
     __shared__ __attribute__((aligned(1024))) uint16_t a1[T::A_EL];
     __shared__ __attribute__((aligned(1024))) uint16_t bl0[T::BL_EL];
@@ -249,26 +287,13 @@ void product_bf16_kernel(ARGS args) {
     __shared__ __attribute__((aligned(1024))) uint16_t bl1[T::BL_EL];
     __shared__ __attribute__((aligned(1024))) uint16_t bh1[T::BH_EL];
     __shared__ __attribute__((aligned(1024))) uint16_t stg[T::S_EL];
-    Tiled<ARGS> p;
-    const uint16_t *a, *b;
-    int M, N, K;
-    if (!place_tile<T, A_KMAJOR, B_KMAJOR>(args, &p, &a, &b, &M, &N, &K)) return;
-    // bytes from the corner on: of a tile's rows, or of a range's k rows
-    const long long lda = args.a.ld, ldb = args.b.ld;
-    const auto ra = make_rsrc(a, record_bytes(2 * (A_KMAJOR ? min(M, T::BM) * lda : K * lda)));
-    const auto rb = make_rsrc(b, record_bytes(2 * (B_KMAJOR ? min(N, T::BN) * ldb : K * ldb)));
-    phase_tile<T, A_KMAJOR, B_KMAJOR, ARGS::OUT, 0>(p, ra, rb, 0, M, N, K, 0, 0, p.t_n, a0, a1, bl0,
-                                                    bh0, bl1, bh1, stg);
-}
-
-template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
-__global__ __launch_bounds__(T::NT) void product_f32_kernel(ARGS args) {
-    __shared__ __attribute__((aligned(1024))) float lds[4 * T::OP_EL];
-    Tiled<ARGS> p;
-    const float *a, *b;
-    int M, N, K;
-    if (!place_tile<T, A_KMAJOR, B_KMAJOR>(args, &p, &a, &b, &M, &N, &K)) return;
-    f32_tile<T, A_KMAJOR, B_KMAJOR>(p, a, b, M, N, K, lds);
+    const int block = blockIdx.x;
+    if constexpr (std::is_same<SECOND, NoProduct>::value) {
+        run_tile<T>(first, block, a0, a1, bl0, bh0, bl1, bh1, stg);
+    } else {
+        if (block < blocks) run_tile<T>(first, block, a0, a1, bl0, bh0, bl1, bh1, stg);
+        else run_tile<T>(second, block - blocks, a0, a1, bl0, bh0, bl1, bh1, stg);
+    }
 }
 
 // ------------------------------------------------------------------ f32 main loop
@@ -324,9 +349,10 @@ struct F32Stage {
 // multiplies k = t and 4 + t. Stages are double-buffered in LDS behind one barrier, the
 // next one's loads in flight in registers. Bound by the matrix instructions (64 cycles
 // each, 32 of them a stage and wave).
-template <class T, bool A_KMAJOR, bool B_KMAJOR, class ARGS>
+template <class T, class ARGS>
 __device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const float* b, int M,
                                          int N, int K, float* lds) {
+    constexpr bool A_KMAJOR = ARGS::A_KMAJOR, B_KMAJOR = ARGS::B_KMAJOR;
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int wm = wave / T::WGN, wn = wave % T::WGN;
     const int fm_live = min(T::FM, max(0, (M - wm * T::WM + 31) / 32));
@@ -668,8 +694,8 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<GradZA
 }
 
 // f32 sums of the tile's range of k, into its slot.
-template <class T, int EPI>
-__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<PartArgs>& p,
+template <class T, int EPI, bool LEFT>
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<PartArgs<LEFT>>& p,
                                             f32x16 (&acc)[T::FM][T::PB], float (&rsum)[T::FM],
                                             bool row_sum, const LdsArrays& arrays, int, int M,
                                             int N, int, int, int fm_live) {
@@ -745,39 +771,19 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StoreA
 
 __device__ __forceinline__ bool is_class(int c, int V) { return c >= 0 && c < V; }
 
-struct MarkArgs {
-    const void* bias;
+// What the rows are told: labels and teacher's lists.
+struct Told {
     const int32_t* labels;
     const int32_t* teacher_idx;
     const float* teacher_logits;
     const float* row_weight;
-    float* row_losses;
-    int32_t* place;   // of live rows: the place among the block's
-    int32_t* counts;  // [row blocks] live rows
-    float* zbias;
-    unsigned* ticket;
-    int N, V, K, vpad, row_blocks, dtype;
+    int N, V, K;
 };
 
-// Blocks [0, row_blocks): a row a thread; the others the bias.
-__global__ __launch_bounds__(kMarkRows) void mark_kernel(MarkArgs p) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
-        const int c = (blockIdx.x - p.row_blocks) * kMarkRows + tid;
-        if (c == 0) *p.ticket = 0;
-        if (c >= p.vpad) return;
-        float v = -__builtin_inff();
-        if (c < p.V) {
-            v = 0.0f;
-            if (p.bias != nullptr)
-                v = p.dtype == VMOE_BF16 ? bf16_to_f32(static_cast<const uint16_t*>(p.bias)[c])
-                                         : static_cast<const float*>(p.bias)[c];
-        }
-        p.zbias[c] = v;
-        return;
-    }
-    __shared__ int wsum[kMarkRows / 64];
-    const int t = blockIdx.x * kMarkRows + tid;
+// Whether row t0 + lane has a label or a teacher and a weight; rows from N on have not.
+// All lanes of a wave together.
+__device__ __forceinline__ bool row_is_live(const Told& p, int t0) {
+    const int lane = threadIdx.x & 63, t = t0 + lane;
     const bool counts = t < p.N && (p.row_weight == nullptr || p.row_weight[t] != 0.0f);
     bool live = counts && p.labels != nullptr && is_class(p.labels[t], p.V);
     // rows without a label: whether their list has an entry. Mostly the first is one;
@@ -799,30 +805,74 @@ __global__ __launch_bounds__(kMarkRows) void mark_kernel(MarkArgs p) {
             open &= open - 1;
         }
         for (int j0 = 0; j0 < p.K; j0 += 64) {
-            const int j = j0 + lane;
-            bool there[U];
+            const int j = min(j0 + lane, p.K - 1);  // (the last entry again does no harm)
+            int c[U];
+            float u[U];
+            bool any = false;
 #pragma unroll
             for (int v = 0; v < U; ++v)
-                there[v] = j < p.K &&
-                           is_class(p.teacher_idx[static_cast<size_t>(t - lane + row[v]) * p.K + j],
-                                    p.V);
+                c[v] = p.teacher_idx[static_cast<size_t>(t0 + row[v]) * p.K + j];
+#pragma unroll
+            for (int v = 0; v < U; ++v) any |= is_class(c[v], p.V);
+            if (!__any(any)) continue;
 #pragma unroll
             for (int v = 0; v < U; ++v)
-                if (there[v])
-                    there[v] = p.teacher_logits[static_cast<size_t>(t - lane + row[v]) * p.K + j] !=
-                               -__builtin_inff();
+                u[v] = p.teacher_logits[static_cast<size_t>(t0 + row[v]) * p.K + j];
 #pragma unroll
-            for (int v = 0; v < U; ++v) found[v] |= __ballot(there[v]);
+            for (int v = 0; v < U; ++v)
+                found[v] |= __ballot(is_class(c[v], p.V) && u[v] != -__builtin_inff());
         }
 #pragma unroll
         for (int v = 0; v < U; ++v) live |= lane == row[v] && found[v] != 0;
     }
+    return live;
+}
+
+// The bias in f32, -infinity past the classes.
+struct BiasArgs {
+    const void* bias;
+    float* zbias;
+    unsigned* ticket;  // cleared beside it
+    int V, vpad, bf16;
+};
+__device__ __forceinline__ void pad_bias(const BiasArgs& p, int c) {
+    if (c == 0) *p.ticket = 0;
+    if (c >= p.vpad) return;
+    float v = -__builtin_inff();
+    if (c < p.V) {
+        v = 0.0f;
+        if (p.bias != nullptr)
+            v = p.bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p.bias)[c])
+                       : static_cast<const float*>(p.bias)[c];
+    }
+    p.zbias[c] = v;
+}
+
+struct MarkArgs {
+    Told told;
+    BiasArgs bias;
+    float* row_losses;
+    int32_t* place;   // of live rows: the place among the block's
+    int32_t* counts;  // [row blocks] live rows
+    int row_blocks;
+};
+
+// Blocks [0, row_blocks): a row a thread; the others the bias.
+__global__ __launch_bounds__(kMarkRows) void mark_kernel(MarkArgs p) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
+        pad_bias(p.bias, (blockIdx.x - p.row_blocks) * kMarkRows + tid);
+        return;
+    }
+    __shared__ int wsum[kMarkRows / 64];
+    const int t = blockIdx.x * kMarkRows + tid;
+    const bool live = row_is_live(p.told, t - lane);
     const uint64_t all = __ballot(live);
     if (lane == 0) wsum[wave] = __popcll(all);
     __syncthreads();
     int before = __popcll(all & ((1ull << lane) - 1));
     for (int w = 0; w < wave; ++w) before += wsum[w];
-    if (t < p.N) {
+    if (t < p.told.N) {
         p.place[t] = live ? before : -1;
         if (!live && p.row_losses != nullptr)
             reinterpret_cast<float2*>(p.row_losses)[t] = make_float2(0.0f, 0.0f);
@@ -842,34 +892,47 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
     v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        v[2 * q] = bf16_to_f32(w[q] & 0xFFFFu);
-        v[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u);
-    }
+
+// Eight results rounded to 16 or 32 bytes.
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+    *reinterpret_cast<uint4*>(p) =
+        make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                   pack_bf16x2(v[6], v[7]));
 }
 
 struct RowArgs {
     const void* x;
-    const int32_t* labels;
-    const int32_t* teacher_idx;
-    const float* teacher_logits;
-    const float* row_weight;
+    Told told;
+    BiasArgs bias;  // FEW
+    float* row_losses;
     const int32_t* counts;
     Saved s;
-    int N, V, K, d, row_blocks, biased;
+    int d, row_blocks, biased;
     float inv_t;
 };
 
-// Rows 4 b .. + 3 of block b, a wave each.
-template <typename E>
+// Rows 4 b .. + 3 of block b, a wave each. FEW (at most 64 rows): every wave marks all
+// of them itself, so that no launch stands before, and blocks behind the rows' take
+// the bias.
+template <typename E, bool FEW>
 __global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
     constexpr int R = (VMOE_HEAD_MAX_TEACHER + 63) / 64;  // entries a lane
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int t = blockIdx.x * 4 + wave, mine = blockIdx.x * 4 / kMarkRows;
+    const int V = p.told.V, K = p.told.K;
+    uint64_t marks = 0;
+    if constexpr (FEW) {
+        const int row_blocks = max(1, (p.told.N + 3) / 4);
+        if (static_cast<int>(blockIdx.x) >= row_blocks) {
+            pad_bias(p.bias, (blockIdx.x - row_blocks) * 256 + threadIdx.x);
+            return;
+        }
+        marks = __ballot(row_is_live(p.told, 0));
+    }
     auto live_before = [&](int blocks) {
         int n = 0;
         for (int b = lane; b < blocks; b += 64) n += p.counts[b];
@@ -878,26 +941,39 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
         return n;
     };
     if (blockIdx.x == 0 && wave == 0) {
-        const int all = live_before(p.row_blocks);
+        const int all = FEW ? __popcll(marks) : live_before(p.row_blocks);
         if (lane == 0) {
             p.s.head->live = all;
-            p.s.head->labelled = p.labels != nullptr;
+            p.s.head->labelled = p.told.labels != nullptr;
             p.s.head->biased = p.biased;
         }
     }
-    if (t >= p.N) return;
-    const int local = p.s.place[t];
-    if (local < 0) return;
-    const int at = local + live_before(mine);
+    if (t >= p.told.N) return;
+    int at;
+    if constexpr (FEW) {
+        if (((marks >> t) & 1) == 0) {
+            if (lane == 0) {
+                p.s.place[t] = -1;
+                if (p.row_losses != nullptr)
+                    reinterpret_cast<float2*>(p.row_losses)[t] = make_float2(0.0f, 0.0f);
+            }
+            return;
+        }
+        at = __popcll(marks & ((1ull << t) - 1));
+    } else {
+        at = p.s.place[t];
+        if (at < 0) return;
+        at += live_before(mine);
+    }
     const E* const x = static_cast<const E*>(p.x) + static_cast<size_t>(t) * p.d;
     E* const xc = static_cast<E*>(p.s.x) + static_cast<size_t>(at) * p.d;
     constexpr int PER = 16 / sizeof(E);
     for (int c = lane * PER; c < p.d; c += 64 * PER)
         *reinterpret_cast<uint4*>(xc + c) = *reinterpret_cast<const uint4*>(x + c);
 
-    const size_t out = static_cast<size_t>(at) * (1 + p.K);
-    const int label = p.labels != nullptr ? p.labels[t] : -1;
-    const bool labelled = is_class(label, p.V);
+    const size_t out = static_cast<size_t>(at) * (1 + K);
+    const int label = p.told.labels != nullptr ? p.told.labels[t] : -1;
+    const bool labelled = is_class(label, V);
     int idx[R];
     float u[R];  // the entries' logits
     float top = -__builtin_inff();
@@ -907,11 +983,11 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
         const int j = lane + 64 * i;
         idx[i] = -1;
         u[i] = 0.0f;
-        if (j < p.K) {
-            const size_t from = static_cast<size_t>(t) * p.K + j;
-            const int c = p.teacher_idx[from];
-            if (is_class(c, p.V)) {
-                u[i] = p.teacher_logits[from];
+        if (j < K) {
+            const size_t from = static_cast<size_t>(t) * K + j;
+            const int c = p.told.teacher_idx[from];
+            if (is_class(c, V)) {
+                u[i] = p.told.teacher_logits[from];
                 if (u[i] != -__builtin_inff()) {
                     idx[i] = c;
                     top = fmaxf(top, u[i]);
@@ -942,14 +1018,14 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
             // (an entry too small to count: not 0 times its logarithm, infinite at worst)
             if (q != 0.0f) inner += q * (u[i] - log_mass);
         }
-        if (j < p.K) {
+        if (j < K) {
             p.s.tidx[out + 1 + j] = idx[i];
             p.s.tq[out + 1 + j] = q;
         }
     }
     inner = wave_total(inner);
     if (lane == 0) {
-        const float w = p.row_weight != nullptr ? p.row_weight[t] : 1.0f;
+        const float w = p.told.row_weight != nullptr ? p.told.row_weight[t] : 1.0f;
         p.s.tidx[out] = labelled ? label : -1;
         p.s.tq[out] = labelled ? 1.0f : 0.0f;
         p.s.row[at] = t;
@@ -1022,6 +1098,211 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs p) {
     });
 }
 
+// ------------------------------------------------------------------ few rows
+
+// At most 64 rows: a block of 256 x 256 tiles would leave most of its waves without a
+// row and most CUs without a tile, each streaming half a megabyte of weights through
+// one CU's share of the bandwidth. Here a block takes all rows against 32 classes: its
+// four waves share k in 128-byte groups, two in flight in registers, which pass through
+// LDS of the wave's own (16-byte chunks XOR-swizzled by row) to be read back as
+// fragments; the waves' sums meet in LDS and are added in wave order.
+constexpr int kFewRows = 64, kFewClasses = 32;
+constexpr int kFewLd = kFewClasses + 4;  // floats a row of z in LDS
+
+template <typename E, int RB>
+struct FewLds {
+    static constexpr int ROWS = 32 * RB + 32, STAGE = ROWS * 128, PART = RB * 16 * 64 * 4;
+    static constexpr int BYTES = 4 * (STAGE > PART ? STAGE : PART);
+};
+
+// z of rows [0, rows) and classes [n0, n0 + 32) into zt (bias and all, -infinity past the
+// classes; rows behind the last hold nothing of use).
+template <typename E, int RB>
+__device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias, int rows, int V,
+                                      int d, int n0, char* lds, float (*zt)[kFewLd]) {
+    constexpr int PER = 16 / sizeof(E), GROUP = 8 * PER;  // elements of a chunk, of a group
+    constexpr int LA = 4 * RB, LB = 4;
+    const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
+    const int lr = lane >> 3, lc = PER * (lane & 7);
+    const int classes = min(kFewClasses, V - n0);
+    const long long row_bytes = static_cast<long long>(d) * sizeof(E);
+    const auto rx = make_rsrc(x, rows * row_bytes);
+    const auto rw = make_rsrc(w + static_cast<size_t>(n0) * d, classes * row_bytes);
+    const int ng = (d + GROUP - 1) / GROUP, g0 = ng * wave / 4, g1 = ng * (wave + 1) / 4;
+    uint4 fa[2][LA], fb[2][LB];
+    auto load = [&](int u, int g) {  // (past the wave's last group nothing is read)
+        const int k = GROUP * g + lc;
+        const bool in = g < g1 && k < d;
+        auto at = [&](int r, int most) {
+            return in && r < most ? static_cast<uint32_t>(r * d + k) * sizeof(E) : kOutOfRange;
+        };
+#pragma unroll
+        for (int i = 0; i < LB; ++i) fb[u][i] = buf_load16(rw, at(8 * i + lr, classes));
+#pragma unroll
+        for (int i = 0; i < LA; ++i) fa[u][i] = buf_load16(rx, at(8 * i + lr, rows));
+    };
+    f32x16 acc[RB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[i][q] = 0.0f;
+    char* const st = lds + wave * FewLds<E, RB>::STAGE;
+    auto at = [&](int r, int c) {
+        return reinterpret_cast<uint4*>(st + r * 128 + ((c ^ (r & 7)) << 4));
+    };
+    load(0, g0);
+    __builtin_amdgcn_sched_barrier(0);
+    load(1, g0 + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    for (int g = g0; g < g1; g += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            // (one wave's LDS accesses run in order: the previous group's reads are
+            // done before these writes)
+#pragma unroll
+            for (int i = 0; i < LA; ++i) *at(8 * i + lr, lane & 7) = fa[u][i];
+#pragma unroll
+            for (int i = 0; i < LB; ++i) *at(32 * RB + 8 * i + lr, lane & 7) = fb[u][i];
+            __builtin_amdgcn_sched_barrier(0);
+            load(u, g + u + 2);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const uint4 b = *at(32 * RB + (lane & 31), 2 * s + h);
+#pragma unroll
+                for (int i = 0; i < RB; ++i) {
+                    const uint4 a = *at(32 * i + (lane & 31), 2 * s + h);
+                    if constexpr (sizeof(E) == 2) {
+                        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            __builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), acc[i], 0,
+                            0, 0);
+                    } else {
+                        const f32x4 av = __builtin_bit_cast(f32x4, a);
+                        const f32x4 bv = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+                            acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(bv[t], av[t], acc[i], 0,
+                                                                          0, 0);
+                    }
+                }
+            }
+        }
+    }
+    __syncthreads();  // every wave is done with its staged rows
+    float* const part = reinterpret_cast<float*>(lds);  // [wave][i][register][lane]
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) part[((wave * RB + i) * 16 + q) * 64 + lane] = acc[i][q];
+    __syncthreads();
+    // wave w: columns 8 w + 4 (lane / 32) + 0..3 of row 32 i + lane % 32
+    const int c = 8 * wave + 4 * h;
+    const float4 bias = *reinterpret_cast<const float4*>(zbias + n0 + c);
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w2 = 0; w2 < 4; ++w2)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                v[q] += part[((w2 * RB + i) * 16 + 4 * wave + q) * 64 + lane];
+        *reinterpret_cast<float4*>(&zt[32 * i + (lane & 31)][c]) =
+            make_float4(v[0] + bias.x, v[1] + bias.y, v[2] + bias.z, v[3] + bias.w);
+    }
+    __syncthreads();
+}
+
+struct FewStatsArgs {
+    Saved s;
+    const void* weight;
+    float *mx, *sum, *sum_t;  // [strips][N]: a strip is a block's classes
+    int N, V, K, d;
+    float scale, scale_t;
+};
+
+template <typename E, int RB>
+__global__ __launch_bounds__(256) void few_stats_kernel(FewStatsArgs p) {
+    __shared__ __attribute__((aligned(16))) char lds[FewLds<E, RB>::BYTES];
+    __shared__ __attribute__((aligned(16))) float zt[32 * RB][kFewLd];
+    const int tid = threadIdx.x, n0 = blockIdx.x * kFewClasses, live = p.s.head->live;
+    if (live == 0) return;
+    few_z<E, RB>(static_cast<const E*>(p.s.x), static_cast<const E*>(p.weight), p.s.bias, live, p.V,
+                 p.d, n0, lds, zt);
+    // four threads a row, eight classes each
+    const int r = tid >> 2, c0 = 8 * (tid & 3);
+    if (r < 32 * RB) {
+        float z[8], m = kLowest;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            z[q] = zt[r][c0 + q];
+            m = fmaxf(m, z[q]);
+        }
+        m = fmaxf(m, __shfl_xor(m, 1, 64));
+        m = fmaxf(m, __shfl_xor(m, 2, 64));
+        auto total = [&](float scale) {
+            const float at = m * scale;  // (as the tiles' sums)
+            float s = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                s += __builtin_amdgcn_exp2f(__builtin_fmaf(z[q], scale, -at));
+            s += __shfl_xor(s, 1, 64);
+            return s + __shfl_xor(s, 2, 64);
+        };
+        const float s = total(p.scale), st = p.sum_t != nullptr ? total(p.scale_t) : 0.0f;
+        const size_t at = static_cast<size_t>(blockIdx.x) * p.N + r;
+        if (r < live && (tid & 3) == 0) {
+            p.mx[at] = m;
+            p.sum[at] = s;
+            if (p.sum_t != nullptr) p.sum_t[at] = st;
+        }
+    }
+    // the logits of the targets among these classes
+    const int n = 1 + p.K;
+#pragma unroll 4
+    for (int e = tid; e < live * n; e += 256) {
+        const int c = p.s.tidx[e];
+        if (c >= n0 && c < n0 + kFewClasses) p.s.tz[e] = zt[e / n][c - n0];
+        else if (c < 0 && blockIdx.x == 0) p.s.tz[e] = 0.0f;
+    }
+}
+
+struct FewGradArgs {
+    Saved s;
+    const void* weight;  // of the piece
+    void* dz;
+    int first, V, K, d, ldz;  // V: classes of the piece
+    int mean;
+    float w_label, w_teacher, inv_t;
+};
+
+template <typename E, int RB>
+__global__ __launch_bounds__(256) void few_grad_kernel(FewGradArgs p) {
+    __shared__ __attribute__((aligned(16))) char lds[FewLds<E, RB>::BYTES];
+    __shared__ __attribute__((aligned(16))) float zt[32 * RB][kFewLd];
+    const int tid = threadIdx.x, n0 = blockIdx.x * kFewClasses;
+    const Header h = *p.s.head;
+    if (h.live == 0) return;
+    few_z<E, RB>(static_cast<const E*>(p.s.x), static_cast<const E*>(p.weight),
+                 p.s.bias + p.first, h.live, p.V, p.d, n0, lds, zt);
+    const int r = tid >> 2, c0 = 8 * (tid & 3);
+    if (r >= h.live) return;
+    const float4 rec = p.s.rec[r];
+    const float2 g = row_rates(h, p.s.weight[r], p.w_label, p.w_teacher, p.mean);
+    const Softmax soft(h, p.K > 0, p.inv_t);
+    // (with a teacher, subtract_kernel sees to the targets)
+    const int label = p.K == 0 ? p.s.tidx[r] - p.first - n0 - c0 : -1;
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const float z = zt[r][c0 + q];
+        v[q] = soft.two ? soft.at<true>(z, rec, g) : soft.at<false>(z, rec, g);
+        if (q == label) v[q] -= g.x;
+    }
+    store8(static_cast<E*>(p.dz) + static_cast<size_t>(r) * p.ldz + n0 + c0, v);
+}
+
+// ------------------------------------------------------------------ losses
+
 struct FinishArgs {
     Saved s;
     const float *mx, *sum, *sum_t;
@@ -1067,7 +1348,7 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     // max z / T and z / T of a target are to be rounded alike: their difference counts
 #pragma clang fp contract(off)
     constexpr int W = kFinishWaves, U = 4;
-    __shared__ float mx_s[W][64], sum_s[W][64], sumt_s[W][64], cross_s[W][64];
+    __shared__ float mx_s[W][64], sum_s[W][64], sumt_s[W][64], cross_s[64];
     __shared__ double part_s[W][4];
     __shared__ bool last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -1076,12 +1357,31 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     const bool in = r < live, two = p.sum_t != nullptr;
     const float scale = kLog2e * p.inv, scale_t = kLog2e * p.inv_t;
     RowSums z;
-    float cross = 0.0f;
+    // sum_j q_j z_j / T of four rows a wave, a lane an entry (z of one that is none is 0)
+    if (p.K > 0) {
+#pragma unroll
+        for (int u = 0; u < 64 / W; ++u) {
+            const int row = blockIdx.x * 64 + wave * (64 / W) + u;
+            const size_t entry = static_cast<size_t>(min(row, max(live - 1, 0))) * (1 + p.K) + 1;
+            float v = 0.0f;
+            for (int j = lane; j < p.K; j += 64)
+                v = __builtin_fmaf(p.s.tq[entry + j], p.s.tz[entry + j] * p.inv_t, v);
+            v = wave_total(v);
+            if (lane == 0) cross_s[wave * (64 / W) + u] = v;
+        }
+    }
+    // (requested ahead of the strips)
+    float2 weight = make_float2(0.0f, 0.0f);
+    float4 rec = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float zlabel = 0.0f;
+    int row = 0;
+    if (wave == 0 && in) {
+        weight = p.s.weight[r];
+        rec = p.s.rec[r];
+        zlabel = p.s.tz[static_cast<size_t>(r) * (1 + p.K)];
+        row = p.s.row[r];
+    }
     if (in) {
-        const size_t entry = static_cast<size_t>(r) * (1 + p.K);
-#pragma unroll 4
-        for (int j = 1 + wave; j <= p.K; j += W)  // (z of an entry that is none is 0)
-            cross = __builtin_fmaf(p.s.tq[entry + j], p.s.tz[entry + j] * p.inv_t, cross);
         for (int q = wave; q < p.strips; q += U * W) {
             float m2[U], s2[U], t2[U];
 #pragma unroll
@@ -1100,7 +1400,6 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     mx_s[wave][lane] = m;
     sum_s[wave][lane] = s;
     sumt_s[wave][lane] = st;
-    cross_s[wave][lane] = cross;
     __syncthreads();
     if (wave == 0) {
         double v[4] = {0.0, 0.0, 0.0, 0.0};
@@ -1111,20 +1410,17 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
                 m2[w - 1] = mx_s[w][lane];
                 s2[w - 1] = sum_s[w][lane];
                 t2[w - 1] = sumt_s[w][lane];
-                cross += cross_s[w][lane];
             }
             z.join<W - 1, false>(m2, s2, t2, scale, scale_t, two);
             m = z.m;
             s = z.s;
             st = z.t;
             if (p.sum_t == nullptr) st = s;
-            const float2 weight = p.s.weight[r];
-            float4 rec = p.s.rec[r];
+            const float cross = p.K > 0 ? cross_s[lane] : 0.0f;
             // (a live row's weight is not 0)
             const bool label = weight.x != 0.0f, taught = weight.y != 0.0f;
             const float lse = m * p.inv + logf(s), lse_t = m * p.inv_t + logf(st);
-            const float a =
-                label ? lse - p.s.tz[static_cast<size_t>(r) * (1 + p.K)] : 0.0f;
+            const float a = label ? lse - zlabel : 0.0f;
             const float tt = p.temperature * p.temperature;
             const float b = taught ? tt * ((rec.w - cross) + lse_t) : 0.0f;
             rec.x = m;
@@ -1132,7 +1428,7 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
             rec.z = log2f(st);
             p.s.rec[r] = rec;
             if (p.row_losses != nullptr)
-                reinterpret_cast<float2*>(p.row_losses)[p.s.row[r]] = make_float2(a, b);
+                reinterpret_cast<float2*>(p.row_losses)[row] = make_float2(a, b);
             v[0] = static_cast<double>(weight.x) * a;
             v[1] = static_cast<double>(weight.y) * b;
             v[2] = weight.x;
@@ -1236,35 +1532,41 @@ __global__ __launch_bounds__(256) void subtract_kernel(SubtractArgs p) {
 }
 
 // dx: the slots' sums, rounded, to the rows' places; zeros for rows left out. Eight
-// columns a thread.
-template <typename E>
+// columns a thread, the slots shared by G of them (many slots stand before few rows,
+// whose threads alone would wait for one after the other).
+template <typename E, int G>
 __global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ part, size_t stride,
                                                  int slots, const int32_t* __restrict__ place,
                                                  E* __restrict__ dx, int N, int d) {
-    const int per = d / 8;
-    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= static_cast<long long>(N) * per) return;
-    const int t = static_cast<int>(i / per), c = 8 * static_cast<int>(i % per), r = place[t];
+    constexpr int PER = 256 / G;
+    __shared__ float sum_s[G > 1 ? G : 1][G > 1 ? PER : 1][8];
+    const int per = d / 8, of = threadIdx.x % PER, g = threadIdx.x / PER;
+    const long long i = static_cast<long long>(blockIdx.x) * PER + of;
+    const bool in = i < static_cast<long long>(N) * per;
+    const int t = in ? static_cast<int>(i / per) : 0, c = 8 * static_cast<int>(i % per);
+    const int r = in ? place[t] : -1;
     float v[8] = {};
     if (r >= 0) {
         const float* at = part + static_cast<size_t>(r) * d + c;
 #pragma unroll 8
-        for (int s = 0; s < slots; ++s) {
+        for (int s = g; s < slots; s += G) {
             float w[8];
             load8(at + s * stride, w);
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] += w[q];
         }
     }
-    E* const out = dx + static_cast<size_t>(t) * d + c;
-    if constexpr (sizeof(E) == 4) {
-        reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-        *reinterpret_cast<uint4*>(out) =
-            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                       pack_bf16x2(v[6], v[7]));
+    if constexpr (G > 1) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum_s[g][of][q] = v[q];
+        __syncthreads();
+        if (g > 0) return;
+#pragma unroll
+        for (int k = 1; k < G; ++k)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] += sum_s[k][of][q];
     }
+    if (in) store8(dx + static_cast<size_t>(t) * d + c, v);
 }
 
 // dW and db of a piece from the slots of its ranges of rows.
@@ -1289,73 +1591,74 @@ __global__ __launch_bounds__(256) void dw_kernel(const float* __restrict__ part,
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] += w[q];
     }
-    E* const out = dw + 8 * i;
-    if constexpr (sizeof(E) == 4) {
-        reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-        *reinterpret_cast<uint4*>(out) =
-            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                       pack_bf16x2(v[6], v[7]));
-    }
+    store8(dw + 8 * i, v);
 }
 
 // ------------------------------------------------------------------ launches
 
-// How a product over M x N with k in `stages` of 64 is cut: the tile's width and the
-// ranges of k.
+// How dx and dW are cut: the tiles' width and the ranges of k of either.
 struct Cut {
-    int narrow, splits;
+    int narrow, dx, dw;
 };
 
-// Time of a cut in units of one CU's 64-deep stage of a 256 x 256 tile (1.8 us): rounds
-// of a tile a CU, each its stages and `extra` for its start and its outputs; more than
-// one range also writes and reads f32 sums (0.06 a tile and range).
-double cut_cost(long long tiles, int stages, int splits, double width, double extra) {
-    const long long rounds = (tiles * splits + kCus - 1) / kCus;
-    const double part = splits > 1 ? 0.06 * width * static_cast<double>(tiles) * splits : 0.0;
-    return static_cast<double>(rounds) * width * ((stages + splits - 1) / splits + extra) + part;
+// `n` blocks of time `t` each, on `cus` CUs that are free at 0, then `n2` blocks of time
+// `t2`: when the last one ends.
+double ends_at(double cus, double n, double t, double n2, double t2) {
+    const double full = floor(n / cus), rest = n - full * cus;  // the last, partial round
+    const double start = full * t;
+    if (n2 <= 0.0) return start + (rest > 0.0 ? t : 0.0);
+    // In time X the CUs without a block of that round take floor(X / t2) of the second
+    // kind, the others floor((X - t) / t2): X is a whole number of t2, or that behind t.
+    const double early = cus - rest, up = ceil(t / t2), down = floor(t / t2);
+    double k = ceil(n2 / early);
+    if (k > up) k = ceil((n2 + rest * up) / cus);
+    const double j = fmax(0.0, ceil((n2 - early * down) / cus));
+    const double x = fmin(k * t2, t + j * t2);
+    return start + (rest > 0.0 ? fmax(x, t) : k * t2);
 }
 
-Cut choose_cut(const vmoe_head_shape& s, long long M, long long N, long long K, int max_splits) {
-    Cut best{0, 1};
-    if (s.dtype != VMOE_BF16) {
-        // 128 x 128, two blocks a CU: four of them for a 256 x 256 tile
-        const long long tiles = ((M + 127) / 128 * ((N + 127) / 128) + 1) / 2;
-        const int stages = static_cast<int>((K + 63) / 64);
-        double least = 1e300;
-        for (int sp = 1; sp <= max_splits && sp <= stages; sp *= 2) {
-            const double c = cut_cost(tiles, stages, sp, 0.5, 1.0);
-            if (c < least) {
-                least = c;
-                best.splits = sp;
-            }
-        }
-        return best;
-    }
-    const long long tm = (M + 255) / 256;
-    const int stages = static_cast<int>((K + 63) / 64);
+// Times are in units of a 64-deep stage of a 256 x 256 tile on one CU (1.8 us): a tile
+// takes its stages, and 8 more for its start and its outputs; f32 sums that are written
+// and read again cost the memory 0.07 a 256 x 256 tile and range. Both products are one
+// launch, dx first.
+Cut choose_cut(const vmoe_head_shape& s, long long cols) {
+    const bool f32 = s.dtype != VMOE_BF16;
+    const long long N = s.n_rows > 0 ? s.n_rows : 1, d = s.d_model;
+    const int sx = static_cast<int>((cols + 63) / 64), sw = static_cast<int>((N + 63) / 64);
+    static const int ranges[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+    Cut best{0, 1, 1};
     double least = 1e300;
-    for (int narrow = 0; narrow < 2; ++narrow) {
-        const int bn = narrow ? 192 : 256;
-        const double width = narrow ? 0.75 * 1.05 : 1.0;
-        for (int sp = 1; sp <= max_splits && sp <= (stages > 0 ? stages : 1); ++sp) {
-            const double c = cut_cost(tm * ((N + bn - 1) / bn), stages, sp, width, 8.0);
-            if (c < least) {
-                least = c;
-                best = Cut{narrow, sp};
+    for (int narrow = 0; narrow < (f32 ? 1 : 2); ++narrow) {
+        const int bm = f32 ? 128 : 256, bn = f32 ? 128 : narrow ? 192 : 256;
+        // (a stage of 128 x 128 in f32 takes as long as two of 256 x 256 in bf16, and two
+        // blocks share a CU)
+        const double stage = f32 ? 2.0 : narrow ? 0.75 * 1.05 : 1.0, extra = f32 ? 1.0 : 8.0;
+        const double cus = f32 ? 2 * kCus : kCus, part = 0.07 * bm * bn / 65536;
+        const double wide = static_cast<double>((d + bn - 1) / bn);
+        const double tx = static_cast<double>((N + bm - 1) / bm) * wide;
+        const double tw = static_cast<double>((cols + bm - 1) / bm) * wide;
+        for (const int x : ranges) {
+            if (x > 1 && (x > sx || tx * x > 6 * cus)) break;
+            const double time_x = stage * ((sx + x - 1) / x + extra);
+            for (const int w : ranges) {
+                if (w > 1 && (w > sw || w > 16 || tw * w > 4 * cus)) break;
+                const double time_w = stage * ((sw + w - 1) / w + extra);
+                const double c = ends_at(cus, tx * x, time_x, tw * w, time_w) +
+                                 part * (tx * x + (w > 1 ? tw * w : 0.0));
+                if (c < least) {
+                    least = c;
+                    best = Cut{narrow, x, w};
+                }
             }
         }
     }
     return best;
 }
 
-constexpr int kMaxDxSplits = 64, kMaxDwSplits = 16;
-
 // The backward's pieces of the classes, and its workspace.
 struct Plan {
     int cols, pieces;  // classes a piece (a multiple of 256)
-    Cut dx, dw;        // of a whole piece
+    Cut cut;
     size_t dz_off, dx_off, dw_off, sums_off, bytes;
 };
 
@@ -1370,8 +1673,7 @@ Plan make_plan(const vmoe_head_shape& s) {
     cols = cols < 256 ? 256 : cols;
     p.pieces = static_cast<int>((vpad + cols - 1) / cols);
     p.cols = static_cast<int>(up256((vpad + p.pieces - 1) / p.pieces));
-    p.dx = choose_cut(s, N, d, p.cols, kMaxDxSplits);
-    p.dw = choose_cut(s, p.cols, d, N, kMaxDwSplits);
+    p.cut = choose_cut(s, p.cols);
     Carver c{nullptr};
     auto take = [&](size_t bytes) {
         const size_t at = c.off;
@@ -1379,9 +1681,9 @@ Plan make_plan(const vmoe_head_shape& s) {
         return at;
     };
     p.dz_off = take(static_cast<size_t>(N) * p.cols * elem_bytes(s));
-    p.dx_off = take(4 * static_cast<size_t>(p.dx.splits) * N * d);
-    p.dw_off = take(p.dw.splits > 1 ? 4 * static_cast<size_t>(p.dw.splits) * p.cols * d : 0);
-    p.sums_off = take(p.dw.splits > 1 ? 4 * static_cast<size_t>(p.dw.splits) * p.cols : 0);
+    p.dx_off = take(4 * static_cast<size_t>(p.cut.dx) * N * d);
+    p.dw_off = take(p.cut.dw > 1 ? 4 * static_cast<size_t>(p.cut.dw) * p.cols * d : 0);
+    p.sums_off = take(p.cut.dw > 1 ? 4 * static_cast<size_t>(p.cut.dw) * p.cols : 0);
     p.bytes = c.off;
     return p;
 }
@@ -1390,7 +1692,7 @@ static_assert(TileBig::BN == 256 && TileBig::WGN == 2 && F32Tile::BN == 128 && F
               "two strips a tile of z");
 
 struct FwdPlan {
-    int row_blocks, strips, finish_blocks, two;
+    int few, row_blocks, strips, finish_blocks, two;
     int tile_rows, tile_shift, tiles_n;  // of z
     size_t counts_off, ticket_off, sums_off, mx_off, sum_off, sumt_off, list_off, ends_off, bytes;
 };
@@ -1402,7 +1704,8 @@ FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     p.tile_rows = s.dtype == VMOE_BF16 ? TileBig::BM : F32Tile::BM;
     p.tile_shift = s.dtype == VMOE_BF16 ? 8 : 7;
     p.tiles_n = static_cast<int>(cdiv(s.n_classes, 1 << p.tile_shift));
-    p.strips = 2 * p.tiles_n;
+    p.few = s.n_rows <= kFewRows;
+    p.strips = p.few ? static_cast<int>(cdiv(s.n_classes, kFewClasses)) : 2 * p.tiles_n;
     p.finish_blocks = s.n_rows > 0 ? static_cast<int>(cdiv(s.n_rows, 64)) : 1;
     p.two = labels && s.n_teacher > 0 && s.temperature != 1.0f;
     Carver c{nullptr};
@@ -1425,26 +1728,39 @@ FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     return p;
 }
 
-template <class T, bool AK, bool BK, class ARGS>
-void launch_product(ARGS a, long long grid_m, hipStream_t st) {
+// Fills in how a product's tiles are dealt to blocks; the blocks it takes.
+template <class T>
+unsigned deal(Product& a, long long grid_m) {
     a.tiles_n = static_cast<int>(cdiv(a.N, T::BN));
     a.group_m = 4;
     a.chunk = 16;
     const long long tiles = static_cast<long long>(cdiv(grid_m, T::BM)) * a.tiles_n * a.splits;
-    if (tiles == 0) return;
-    const unsigned grid = 8 * cdiv(tiles, 8 * a.chunk) * a.chunk;
-    if constexpr (is_f32<T>())
-        product_f32_kernel<T, AK, BK><<<grid, T::NT, 0, st>>>(a);
-    else
-        product_bf16_kernel<T, AK, BK><<<grid, T::NT, 0, st>>>(a);
+    return 8 * cdiv(tiles, 8 * a.chunk) * a.chunk;
+}
+template <class T>
+unsigned deal(NoProduct&, long long) { return 0; }
+
+template <class T, class FIRST, class SECOND>
+void launch_products(FIRST a, long long rows_a, SECOND b, long long rows_b, hipStream_t st) {
+    const unsigned na = rows_a > 0 ? deal<T>(a, rows_a) : 0;
+    const unsigned nb = rows_b > 0 ? deal<T>(b, rows_b) : 0;
+    if (na + nb > 0) product_kernel<T><<<na + nb, T::NT, 0, st>>>(a, b, static_cast<int>(na));
 }
 
-template <bool AK, bool BK, class ARGS>
-void launch_product(const vmoe_head_shape& s, int narrow, const ARGS& a, long long grid_m,
-                    hipStream_t st) {
-    if (s.dtype != VMOE_BF16) launch_product<F32Tile, AK, BK>(a, grid_m, st);
-    else if (narrow) launch_product<TileNarrow, AK, BK>(a, grid_m, st);
-    else launch_product<TileBig, AK, BK>(a, grid_m, st);
+// rows_a, rows_b: the products' m (0: not formed).
+template <class FIRST, class SECOND>
+void launch_products(const vmoe_head_shape& s, int narrow, const FIRST& a, long long rows_a,
+                     const SECOND& b, long long rows_b, hipStream_t st) {
+    if (s.dtype != VMOE_BF16) launch_products<F32Tile>(a, rows_a, b, rows_b, st);
+    else if (narrow) launch_products<TileNarrow>(a, rows_a, b, rows_b, st);
+    else launch_products<TileBig>(a, rows_a, b, rows_b, st);
+}
+
+// z, whose strips are those of 256 x 256 tiles.
+template <class ARGS>
+void launch_logits(const vmoe_head_shape& s, const ARGS& a, hipStream_t st) {
+    if (s.dtype != VMOE_BF16) launch_products<F32Tile>(a, a.M, NoProduct{}, 0, st);
+    else launch_products<TileBig>(a, a.M, NoProduct{}, 0, st);
 }
 
 }  // namespace
@@ -1461,49 +1777,68 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
     const FwdPlan p = make_fwd_plan(s, labels != nullptr);
     char* const base = static_cast<char*>(ws);
     const int N = s.n_rows, V = s.n_classes, K = s.n_teacher;
-    MarkArgs m{bias, labels, teacher_idx, teacher_logits, row_weight, row_losses, v.place,
-               reinterpret_cast<int32_t*>(base + p.counts_off), v.bias,
-               reinterpret_cast<unsigned*>(base + p.ticket_off), N, V, K, padded_classes(s),
-               p.row_blocks, s.dtype};
-    mark_kernel<<<p.row_blocks + cdiv(padded_classes(s), kMarkRows), kMarkRows, 0, st>>>(m);
+    const Told told{labels, teacher_idx, teacher_logits, row_weight, N, V, K};
+    const BiasArgs zb{bias, v.bias, reinterpret_cast<unsigned*>(base + p.ticket_off), V,
+                      padded_classes(s), s.dtype == VMOE_BF16};
+    const MarkArgs m{told, zb, row_losses, v.place,
+                     reinterpret_cast<int32_t*>(base + p.counts_off), p.row_blocks};
+    const bool bf16 = s.dtype == VMOE_BF16;
     const float inv_t = 1.0f / s.temperature;
-    const RowArgs t{x, labels, teacher_idx, teacher_logits, row_weight, m.counts, v,
-                    N, V, K, s.d_model, p.row_blocks, bias != nullptr, inv_t};
+    const RowArgs t{x, told, zb, row_losses, m.counts, v, s.d_model, p.row_blocks, bias != nullptr,
+                    inv_t};
     const unsigned row_grid = N > 0 ? cdiv(N, 4) : 1;
-    if (s.dtype == VMOE_BF16) rows_kernel<uint16_t><<<row_grid, 256, 0, st>>>(t);
-    else rows_kernel<float><<<row_grid, 256, 0, st>>>(t);
-    const SortArgs g{v, reinterpret_cast<uint32_t*>(base + p.list_off),
-                     reinterpret_cast<int32_t*>(base + p.ends_off), K, p.tile_rows, p.tile_shift,
-                     p.tiles_n};
-    if (N > 0 && K > 0) sort_kernel<<<cdiv(N, p.tile_rows), 1024, 0, st>>>(g);
+    float* const mx = reinterpret_cast<float*>(base + p.mx_off);
+    float* const sum = reinterpret_cast<float*>(base + p.sum_off);
+    float* const sum_t = p.two ? reinterpret_cast<float*>(base + p.sumt_off) : nullptr;
+    const float inv = K > 0 && labels == nullptr ? inv_t : 1.0f;  // of `sum`
+    if (p.few) {
+        const unsigned grid = row_grid + cdiv(zb.vpad, 256);
+        if (bf16) rows_kernel<uint16_t, true><<<grid, 256, 0, st>>>(t);
+        else rows_kernel<float, true><<<grid, 256, 0, st>>>(t);
+        const FewStatsArgs a{v, weight, mx, sum, sum_t, N, V, K, s.d_model, kLog2e * inv,
+                             kLog2e * inv_t};
+        auto go = [&](auto blocks) {
+            constexpr int RB = decltype(blocks)::value;
+            if (bf16) few_stats_kernel<uint16_t, RB><<<p.strips, 256, 0, st>>>(a);
+            else few_stats_kernel<float, RB><<<p.strips, 256, 0, st>>>(a);
+        };
+        if (N <= 32) go(std::integral_constant<int, 1>{});
+        else go(std::integral_constant<int, 2>{});
+    } else {
+        mark_kernel<<<p.row_blocks + cdiv(zb.vpad, kMarkRows), kMarkRows, 0, st>>>(m);
+        if (bf16) rows_kernel<uint16_t, false><<<row_grid, 256, 0, st>>>(t);
+        else rows_kernel<float, false><<<row_grid, 256, 0, st>>>(t);
+        const SortArgs g{v, reinterpret_cast<uint32_t*>(base + p.list_off),
+                         reinterpret_cast<int32_t*>(base + p.ends_off), K, p.tile_rows,
+                         p.tile_shift, p.tiles_n};
+        if (K > 0) sort_kernel<<<cdiv(N, p.tile_rows), 1024, 0, st>>>(g);
+        StatsArgs a{};
+        a.a = Operand{v.x, 0, s.d_model};
+        a.b = Operand{weight, 0, s.d_model};
+        a.M = N;
+        a.N = V;
+        a.K = s.d_model;
+        a.live = &v.head->live;
+        a.splits = 1;
+        a.zbias = v.bias;
+        a.mx = mx;
+        a.sum = sum;
+        a.sum_t = sum_t;
+        a.tidx = v.tidx;
+        a.tz = v.tz;
+        a.list = K > 0 ? g.list : nullptr;
+        a.ends = g.ends;
+        a.n_rows = N;
+        a.per_row = 1 + K;
+        a.has_bias = bias != nullptr;
+        a.scale_t = kLog2e * inv_t;
+        a.scale = kLog2e * inv;
+        launch_logits(s, a, st);
+    }
 
-    StatsArgs a{};
-    a.a = Operand{v.x, 0, s.d_model};
-    a.b = Operand{weight, 0, s.d_model};
-    a.M = N;
-    a.N = V;
-    a.K = s.d_model;
-    a.live = &v.head->live;
-    a.splits = 1;
-    a.zbias = v.bias;
-    a.mx = reinterpret_cast<float*>(base + p.mx_off);
-    a.sum = reinterpret_cast<float*>(base + p.sum_off);
-    a.sum_t = p.two ? reinterpret_cast<float*>(base + p.sumt_off) : nullptr;
-    a.tidx = v.tidx;
-    a.tz = v.tz;
-    a.list = K > 0 ? g.list : nullptr;
-    a.ends = g.ends;
-    a.n_rows = N;
-    a.per_row = 1 + K;
-    a.has_bias = bias != nullptr;
-    a.scale_t = kLog2e * inv_t;
-    a.scale = K > 0 && labels == nullptr ? a.scale_t : kLog2e;
-    launch_product<true, true>(s, 0, a, N, st);
-
-    const FinishArgs f{v, a.mx, a.sum, a.sum_t,
-                       reinterpret_cast<double*>(base + p.sums_off), m.ticket,
-                 losses, row_losses, p.strips, N, K, s.reduction == VMOE_REDUCE_MEAN,
-                 s.temperature, K > 0 && labels == nullptr ? inv_t : 1.0f, inv_t};
+    const FinishArgs f{v, mx, sum, sum_t, reinterpret_cast<double*>(base + p.sums_off), zb.ticket,
+                       losses, row_losses, p.strips, N, K, s.reduction == VMOE_REDUCE_MEAN,
+                       s.temperature, inv, inv_t};
     finish_kernel<<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
     return launch_status();
 }
@@ -1517,7 +1852,6 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
     const int N = s.n_rows, V = s.n_classes, d = s.d_model;
     const size_t size = elem_bytes(s);
     const bool bf16 = s.dtype == VMOE_BF16;
-    const bool params = dweight != nullptr || dbias != nullptr;
     for (int i = 0; i < p.pieces; ++i) {
         const int first = i * p.cols, count = min(p.cols, V - first);
         if (count <= 0) break;
@@ -1544,7 +1878,20 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
         z.teacher = s.n_teacher > 0;
         z.label = z.teacher ? nullptr : v.tidx;
         z.first = first;
-        launch_product<true, true>(s, 0, z, N, st);
+        if (N <= kFewRows) {
+            const FewGradArgs u{v, w, z.dz, first, count, s.n_teacher, d, z.ldz, z.mean,
+                                z.w_label, z.w_teacher, z.inv_t};
+            const unsigned grid = cdiv(count, kFewClasses);
+            auto go = [&](auto blocks) {
+                constexpr int RB = decltype(blocks)::value;
+                if (bf16) few_grad_kernel<uint16_t, RB><<<grid, 256, 0, st>>>(u);
+                else few_grad_kernel<float, RB><<<grid, 256, 0, st>>>(u);
+            };
+            if (N <= 32) go(std::integral_constant<int, 1>{});
+            else go(std::integral_constant<int, 2>{});
+        } else {
+            launch_logits(s, z, st);
+        }
         if (N > 0 && z.teacher) {
             const SubtractArgs u{v, z.dz, z.ldz, first, count, s.n_teacher, z.mean, z.teacher,
                                  z.w_label, z.w_teacher, z.inv_t};
@@ -1556,75 +1903,76 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             if (s.n_teacher < 64) go(std::integral_constant<int, 1>{});
             else go(std::integral_constant<int, (VMOE_HEAD_MAX_TEACHER + 64) / 64>{});
         }
-        if (dx != nullptr) {
-            PartArgs a{};
-            a.a = Operand{z.dz, 0, z.ldz};
-            a.b = Operand{w, 0, d};
-            a.M = N;
-            a.N = d;
-            a.K = count;
-            a.live = z.live;
-            a.splits = p.dx.splits;
-            a.part = reinterpret_cast<float*>(base + p.dx_off);
-            a.part_stride = static_cast<size_t>(N) * d;
-            a.add = i > 0;
-            launch_product<true, false>(s, p.dx.narrow, a, N, st);
-        }
-        if (params) {
-            Product a{};
-            a.a = Operand{z.dz, 0, z.ldz};
-            a.b = Operand{v.x, 0, d};
-            a.M = count;
-            // (dbias alone: the product with x's first columns, whose tiles sum dz)
-            a.N = dweight != nullptr ? d : 8;
-            a.K = N;
-            a.live = z.live;
-            a.rows_are_k = 1;
-            a.splits = dweight != nullptr ? p.dw.splits : 1;
-            char* const dwp = dweight != nullptr ? static_cast<char*>(dweight) +
-                                                       static_cast<size_t>(first) * d * size
-                                                 : nullptr;
-            char* const dbp =
-                dbias != nullptr ? static_cast<char*>(dbias) + static_cast<size_t>(first) * size
-                                 : nullptr;
-            if (a.splits == 1) {
-                StoreArgs c{};
-                static_cast<Product&>(c) = a;
-                c.c = dwp;
-                c.sums = dbp;
-                c.bsum = static_cast<float*>(c.sums);
-                launch_product<false, false>(s, p.dw.narrow, c, count, st);
-            } else {
-                PartArgs c{};
-                static_cast<Product&>(c) = a;
-                c.part = reinterpret_cast<float*>(base + p.dw_off);
-                c.part_stride = static_cast<size_t>(count) * d;
-                c.part_sums =
-                    dbp != nullptr ? reinterpret_cast<float*>(base + p.sums_off) : nullptr;
-                c.bsum = c.part_sums;
-                launch_product<false, false>(s, p.dw.narrow, c, count, st);
-                const unsigned grid = cdiv(static_cast<long long>(count) * (d / 8), 256);
-                if (bf16)
-                    dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, a.splits,
-                                                    reinterpret_cast<uint16_t*>(dwp),
-                                                    reinterpret_cast<uint16_t*>(dbp), count, d);
-                else
-                    dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, a.splits,
-                                                    reinterpret_cast<float*>(dwp),
-                                                    reinterpret_cast<float*>(dbp), count, d);
-            }
+        PartArgs<true> l{};
+        l.a = Operand{z.dz, 0, z.ldz};
+        l.b = Operand{w, 0, d};
+        l.M = N;
+        l.N = d;
+        l.K = count;
+        l.live = z.live;
+        l.splits = p.cut.dx;
+        l.part = reinterpret_cast<float*>(base + p.dx_off);
+        l.part_stride = static_cast<size_t>(N) * d;
+        l.add = i > 0;
+        Product r{};
+        r.a = Operand{z.dz, 0, z.ldz};
+        r.b = Operand{v.x, 0, d};
+        r.M = count;
+        // (dbias alone: the product with x's first columns, whose tiles sum dz)
+        r.N = dweight != nullptr ? d : 8;
+        r.K = N;
+        r.live = z.live;
+        r.rows_are_k = 1;
+        r.splits = dweight != nullptr ? p.cut.dw : 1;
+        char* const dwp = dweight != nullptr
+                              ? static_cast<char*>(dweight) + static_cast<size_t>(first) * d * size
+                              : nullptr;
+        char* const dbp = dbias != nullptr
+                              ? static_cast<char*>(dbias) + static_cast<size_t>(first) * size
+                              : nullptr;
+        const long long rows_l = dx != nullptr ? N : 0;
+        const long long rows_r = dweight != nullptr || dbias != nullptr ? count : 0;
+        if (r.splits == 1) {
+            StoreArgs c{};
+            static_cast<Product&>(c) = r;
+            c.c = dwp;
+            c.sums = dbp;
+            c.bsum = reinterpret_cast<float*>(dbp);
+            launch_products(s, p.cut.narrow, l, rows_l, c, rows_r, st);
+        } else {
+            PartArgs<false> c{};
+            static_cast<Product&>(c) = r;
+            c.part = reinterpret_cast<float*>(base + p.dw_off);
+            c.part_stride = static_cast<size_t>(count) * d;
+            c.part_sums = dbp != nullptr ? reinterpret_cast<float*>(base + p.sums_off) : nullptr;
+            c.bsum = c.part_sums;
+            launch_products(s, p.cut.narrow, l, rows_l, c, rows_r, st);
+            const unsigned grid = cdiv(static_cast<long long>(count) * (d / 8), 256);
+            if (bf16)
+                dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, r.splits,
+                                                reinterpret_cast<uint16_t*>(dwp),
+                                                reinterpret_cast<uint16_t*>(dbp), count, d);
+            else
+                dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, r.splits,
+                                                reinterpret_cast<float*>(dwp),
+                                                reinterpret_cast<float*>(dbp), count, d);
         }
     }
     if (dx != nullptr && N > 0) {
-        const unsigned grid = cdiv(static_cast<long long>(N) * (d / 8), 256);
         const float* const part = reinterpret_cast<const float*>(base + p.dx_off);
         const size_t stride = static_cast<size_t>(N) * d;
-        if (bf16)
-            dx_kernel<<<grid, 256, 0, st>>>(part, stride, p.dx.splits, v.place,
-                                            static_cast<uint16_t*>(dx), N, d);
-        else
-            dx_kernel<<<grid, 256, 0, st>>>(part, stride, p.dx.splits, v.place,
-                                            static_cast<float*>(dx), N, d);
+        auto go = [&](auto groups) {
+            constexpr int G = decltype(groups)::value;
+            const unsigned grid = cdiv(static_cast<long long>(N) * (d / 8), 256 / G);
+            if (bf16)
+                dx_kernel<uint16_t, G><<<grid, 256, 0, st>>>(part, stride, p.cut.dx, v.place,
+                                                             static_cast<uint16_t*>(dx), N, d);
+            else
+                dx_kernel<float, G><<<grid, 256, 0, st>>>(part, stride, p.cut.dx, v.place,
+                                                          static_cast<float*>(dx), N, d);
+        };
+        if (p.cut.dx >= 16) go(std::integral_constant<int, 8>{});
+        else go(std::integral_constant<int, 1>{});
     }
     return launch_status();
 }
