@@ -26,7 +26,8 @@ typedef enum { VMOE_REDUCE_MEAN = 0, VMOE_REDUCE_SUM = 1 } vmoe_reduction;
 
 typedef struct vmoe_head_shape {
     int32_t n_rows;      /* N >= 0, at most 2^21 (else UNSUPPORTED)                   */
-    int32_t d_model;     /* d, multiple of 8, at most 65536; N d < 2^30 (else UNSUPPORTED) */
+    int32_t d_model;     /* d, multiple of 8, at most 65536; x below 2 GiB (else
+                            UNSUPPORTED)                                              */
     int32_t n_classes;   /* V >= 1, at most 2^21; N V < 2^36 (else UNSUPPORTED)       */
     int32_t n_teacher;   /* K in [0, 256]: entries of the teacher's list; 0: none     */
     int32_t dtype;       /* x, weight, bias and every gradient (vmoe_dtype)           */

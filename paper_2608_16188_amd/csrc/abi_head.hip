@@ -21,7 +21,7 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
 namespace {
 
 constexpr int kMaxRows = 1 << 21, kMaxClasses = 1 << 21, kMaxWidth = 1 << 16;
-constexpr long long kMaxTokens = 1LL << 30;   // N d: 32-bit byte offsets in bf16 rows
+constexpr long long kMaxTokenBytes = 1LL << 31;  // N d: 32-bit offsets
 constexpr long long kMaxLogits = 1LL << 36;   // N V: threads of one launch
 constexpr float kMaxTemperature = 1024.0f;
 
@@ -37,7 +37,7 @@ vmoe_status check_shape(const vmoe_head_shape* s) {
         return VMOE_ERR_INVALID_ARG;
     const long long n = s->n_rows;
     if (s->n_rows > kMaxRows || s->n_classes > kMaxClasses || s->d_model > kMaxWidth ||
-        n * s->d_model >= kMaxTokens || n * s->n_classes >= kMaxLogits)
+        n * s->d_model * (s->dtype == VMOE_BF16 ? 2 : 4) >= kMaxTokenBytes || n * s->n_classes >= kMaxLogits)
         return VMOE_ERR_UNSUPPORTED;
     return VMOE_OK;
 }

@@ -103,14 +103,14 @@ Saved saved_layout(const vmoe_head_shape& s, void* base) {
 
 // ------------------------------------------------------------------ tilings
 
-// f32: 128 x 128 tiles of four waves as 2 x 2, 16-deep stages; a wave's rows and
-// columns lie in the tile as in the phased bf16 tiles (64 wm + 32 i, 64 b + 32 wn).
+// f32: 64 x 128 tiles of four waves as 2 x 2, 32-deep stages; a wave's rows and columns
+// lie in the tile as in the phased bf16 tiles (WM wm + 32 i, 64 b + 32 wn).
 struct F32Tile {
-    static constexpr int PB = 2, BM = 128, BN = 128, WGN = 2, NT = 256, FM = 2, WM = 64;
-    static constexpr int WAVES_PER_EU = 4;
-    static constexpr int KB = 16, OP_EL = BM * KB;
-    // LDS: two stages of both operands, in S_EL (16-bit words)
-    static constexpr int A_EL = 1, BL_EL = 1, BH_EL = 1, S_EL = 4 * OP_EL * 2;
+    static constexpr int PB = 2, BM = 64, BN = 128, WGN = 2, NT = 256, FM = 1, WM = 32;
+    static constexpr int WAVES_PER_EU = 2;
+    static constexpr int KB = 32, A_OP = BM * KB, B_OP = BN * KB;
+    // LDS: two stages of both operands, a0 and a1 (16-bit words)
+    static constexpr int A_EL = (A_OP + B_OP) * 2, BL_EL = 8, BH_EL = 8, S_EL = 8;
 };
 using TileBig = PhaseTile<4>;
 using TileNarrow = PhaseTile<3>;
@@ -214,7 +214,7 @@ __device__ __forceinline__ uint32_t record_bytes(long long bytes) {
 
 template <class T, class ARGS>
 __device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const float* b, int M,
-                                         int N, int K, float* lds);
+                                         int N, int K, float* lds0, float* lds1);
 
 // One tile: the operands are taken from the tile's corner and its range of k on, so that
 // offsets inside it fit 32 bits however large they are.
@@ -259,7 +259,7 @@ __device__ __forceinline__ void run_tile(const ARGS& args, int block, uint16_t* 
     int M, N, K;
     if (!place_tile<T>(args, block, &p, &a, &b, &M, &N, &K)) return;
     if constexpr (is_f32<T>()) {
-        f32_tile<T>(p, a, b, M, N, K, reinterpret_cast<float*>(stg));
+        f32_tile<T>(p, a, b, M, N, K, reinterpret_cast<float*>(a0), reinterpret_cast<float*>(a1));
     } else {
         constexpr bool AK = ARGS::A_KMAJOR, BK = ARGS::B_KMAJOR;
         // bytes from the corner on: of a tile's rows, or of a range's k rows
@@ -298,61 +298,55 @@ void product_kernel(FIRST first, SECOND second, int blocks) {
 
 // ------------------------------------------------------------------ f32 main loop
 
-// One stage of an operand: 128 rows (or columns) by 16 k, two float4 a thread, zero
-// outside. k-major in LDS: 16-byte chunk c of row r at chunk c ^ (r / 4 mod 4);
-// mn-major: k row k, its columns XOR 32 (k / 4 mod 2), so that the halves of a wave
-// read other banks.
-template <bool KMAJOR>
+// A stage of an f32 operand, ROWS rows (or columns) by 32 k, is that of a bf16 operand
+// twice as long in its contiguous direction: 128-byte rows of 8 chunks where k is
+// contiguous, k rows of 4 ROWS bytes where it is not.
+template <bool KMAJOR, int ROWS, int NT>
 struct F32Stage {
-    float4 v[2];
-    __device__ __forceinline__ void load(const float* base, int ld, int lim, int k0, int K) {
-        const int tid = threadIdx.x;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            int mn, k;
-            if constexpr (KMAJOR) { mn = 64 * u + (tid >> 2); k = k0 + 4 * (tid & 3); }
-            else { mn = 4 * (tid & 31); k = k0 + 8 * u + (tid >> 5); }
-            v[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (mn < lim && k < K)
-                v[u] = *reinterpret_cast<const float4*>(
-                    base + (KMAJOR ? static_cast<size_t>(mn) * ld + k
-                                   : static_cast<size_t>(k) * ld + mn));
-        }
+    using Dma = typename std::conditional<KMAJOR, DmaStage<ROWS, true, 64, NT>,
+                                          DmaStage<2 * ROWS, false, 32, NT>>::type;
+    __amdgpu_buffer_rsrc_t rs;
+    int ld, lim, K;
+    uint32_t step, off[Dma::PER];
+    __device__ __forceinline__ F32Stage(const float* base, int ld_, int lim_, int K_)
+        : rs(make_rsrc(base, record_bytes(4LL * (KMAJOR ? lim_ : K_) * ld_))), ld(2 * ld_),
+          lim(KMAJOR ? lim_ : 2 * lim_), K(KMAJOR ? 2 * K_ : K_),
+          step(KMAJOR ? 128u : 128u * static_cast<uint32_t>(ld_)) {
+        Dma::lane_offs(ld, 0, lim, off);
     }
-    __device__ __forceinline__ void put(float* s) const {
-        const int tid = threadIdx.x;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if constexpr (KMAJOR) {
-                const int r = 64 * u + (tid >> 2), c = tid & 3;
-                *reinterpret_cast<float4*>(s + r * 16 + ((c ^ ((r >> 2) & 3)) << 2)) = v[u];
-            } else {
-                const int k = 8 * u + (tid >> 5), c = 4 * (tid & 31);
-                *reinterpret_cast<float4*>(s + k * 128 + (c ^ (((k >> 2) & 1) << 5))) = v[u];
-            }
-        }
+    __device__ __forceinline__ void issue(int kt, float* s) const {
+        uint16_t* const d = reinterpret_cast<uint16_t*>(s);
+        constexpr int KB = KMAJOR ? 64 : 32;
+        if ((kt + 1) * KB <= K) Dma::issue_inside(rs, off, kt * step, d);
+        else Dma::issue(rs, ld, 0, lim, kt * KB, K, d);
     }
     // four k of the lane's half (8 g + 4 (lane / 32) ..) of row mn0 + lane % 32
     static __device__ __forceinline__ float4 frag(const float* s, int mn0, int g, int lane) {
         const int mn = mn0 + (lane & 31), h = lane >> 5;
         if constexpr (KMAJOR) {
             return *reinterpret_cast<const float4*>(
-                s + mn * 16 + (((2 * g + h) ^ ((mn >> 2) & 3)) << 2));
+                s + mn * 32 + (((2 * g + h) ^ ((mn >> 1) & 7)) << 2));
         } else {
-            const float* q = s + (8 * g + 4 * h) * 128 + (mn ^ (h << 5));
-            return make_float4(q[0], q[128], q[256], q[384]);
+            float v[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                v[t] = s[(8 * g + 4 * h + t) * ROWS +
+                         (((mn >> 2) ^ mn_swizzle<2 * ROWS>(t)) << 2) + (mn & 3)];
+            return make_float4(v[0], v[1], v[2], v[3]);
         }
     }
 };
 
 // v_mfma_f32_32x32x2f32 takes one k from either half of the lanes: of eight k, product t
-// multiplies k = t and 4 + t. Stages are double-buffered in LDS behind one barrier, the
-// next one's loads in flight in registers. Bound by the matrix instructions (64 cycles
-// each, 32 of them a stage and wave).
+// multiplies k = t and 4 + t. Two stages in LDS, filled by loads that write it directly;
+// one barrier a stage, behind which the next is requested. Bound by the matrix
+// instructions (64 cycles each).
 template <class T, class ARGS>
 __device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const float* b, int M,
-                                         int N, int K, float* lds) {
+                                         int N, int K, float* lds0, float* lds1) {
     constexpr bool A_KMAJOR = ARGS::A_KMAJOR, B_KMAJOR = ARGS::B_KMAJOR;
+    using SA = F32Stage<A_KMAJOR, T::BM, T::NT>;
+    using SB = F32Stage<B_KMAJOR, T::BN, T::NT>;
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int wm = wave / T::WGN, wn = wave % T::WGN;
     const int fm_live = min(T::FM, max(0, (M - wm * T::WM + 31) / 32));
@@ -367,32 +361,24 @@ __device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const fl
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
     }
-    F32Stage<A_KMAJOR> sa;
-    F32Stage<B_KMAJOR> sb;
     // (mn-major columns come four at a time and the operands' rows are padded, so the
     // last four may pass the limit: their outputs are not stored)
-    const int lim_a = min(M, T::BM), lim_b = min(N, T::BN);
-    sa.load(a, p.a.ld, lim_a, 0, K);
-    sb.load(b, p.b.ld, lim_b, 0, K);
-    for (int k0 = 0, buf = 0; k0 < K; k0 += T::KB, buf ^= 1) {
-        float* const as = lds + buf * 2 * T::OP_EL;
-        float* const bs = as + T::OP_EL;
-        sa.put(as);
-        sb.put(bs);
-        __syncthreads();
-        if (k0 + T::KB < K) {
-            sa.load(a, p.a.ld, lim_a, k0 + T::KB, K);
-            sb.load(b, p.b.ld, lim_b, k0 + T::KB, K);
-        }
+    const SA sa(a, p.a.ld, min(M, T::BM), K);
+    const SB sb(b, p.b.ld, min(N, T::BN), K);
+    const int nk = (K + T::KB - 1) / T::KB;
+    auto request = [&](int kt, float* s) {
+        sa.issue(kt, s);
+        sb.issue(kt, s + T::A_OP);
+    };
+    auto multiply = [&](const float* as) {
+        const float* const bs = as + T::A_OP;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
+        for (int g = 0; g < T::KB / 8; ++g) {
             float4 fa[T::FM], fb[T::PB];
 #pragma unroll
-            for (int i = 0; i < T::FM; ++i)
-                fa[i] = F32Stage<A_KMAJOR>::frag(as, 64 * wm + 32 * i, g, lane);
+            for (int i = 0; i < T::FM; ++i) fa[i] = SA::frag(as, T::WM * wm + 32 * i, g, lane);
 #pragma unroll
-            for (int j = 0; j < T::PB; ++j)
-                fb[j] = F32Stage<B_KMAJOR>::frag(bs, 64 * j + 32 * wn, g, lane);
+            for (int j = 0; j < T::PB; ++j) fb[j] = SB::frag(bs, 64 * j + 32 * wn, g, lane);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -409,11 +395,24 @@ __device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const fl
                     }
                 }
         }
+    };
+    if (nk > 0) request(0, lds0);
+    // (the stage has landed, and this wave's reads of the other buffer are done, before
+    // the barrier; every wave's are behind it)
+    auto stage = [&](int kt, float* cur, float* next) {
+        __builtin_amdgcn_s_waitcnt(VmWait<0>::imm);
+        ring_barrier();
+        if (kt + 1 < nk) request(kt + 1, next);
+        multiply(cur);
+    };
+    for (int kt = 0; kt < nk; kt += 2) {
+        stage(kt, lds0, lds1);
+        if (kt + 1 < nk) stage(kt + 1, lds1, lds0);
     }
     __syncthreads();  // the stages are read: the outputs pass through their LDS
     finish_tile(TileKind<T, ARGS::OUT>{}, p, acc, rsum, row_sum,
                 LdsArrays{nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
-                          reinterpret_cast<uint16_t*>(lds)},
+                          reinterpret_cast<uint16_t*>(lds0)},
                 0, M, N, 0, 0, fm_live);
 }
 
@@ -527,7 +526,7 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsA
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         if (i >= fm_live) break;
-        const int r0 = 64 * wm + 32 * i;
+        const int r0 = T::WM * wm + 32 * i;
         const size_t row = p.t_m0 + min(r0 + (lane & 31), M - 1);
         const int spot = class_spot<T>(p.tidx[row * p.per_row], p.t_n0);
         float m = kLowest;
@@ -577,8 +576,8 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsA
     for (int e0 = from; e0 < to; e0 += 64) {
         const uint32_t e = e0 + lane < to ? list[e0 + lane] : 0;
         const int r = e & 255, c = (e >> 8) & 255;
-        const bool mine = e0 + lane < to && (r >> 6) == wm && ((c >> 5) & 1) == wn;
-        const int block = mine ? ((r >> 5) & 1) * T::PB + (c >> 6) : -1;
+        const bool mine = e0 + lane < to && r / T::WM == wm && ((c >> 5) & 1) == wn;
+        const int block = mine ? r % T::WM / 32 * T::PB + (c >> 6) : -1;
 #pragma unroll
         for (int i = 0; i < T::FM; ++i)
 #pragma unroll
@@ -643,7 +642,7 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<GradZA
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         if (i >= fm_live) break;
-        const int r0 = 64 * wm + 32 * i, r = p.t_m0 + min(r0 + (lane & 31), M - 1);
+        const int r0 = T::WM * wm + 32 * i, r = p.t_m0 + min(r0 + (lane & 31), M - 1);
         const float4 rec = p.rec[r];
         const float2 g = row_rates(h, p.weight[r], p.w_label, p.w_teacher, p.mean);
         const int spot = p.label != nullptr ? class_spot<T>(p.label[r] - p.first, p.t_n0) : -1;
@@ -705,7 +704,7 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<PartAr
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         if (i >= fm_live) break;
-        const int r0 = 64 * wm + 32 * i;
+        const int r0 = T::WM * wm + 32 * i;
         if (row_sum) {
             const float t = rsum[i] + __shfl_xor(rsum[i], 32, 64);
             if (lane < 32 && r0 + lane < M)
@@ -749,7 +748,7 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StoreA
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         if (i >= fm_live) break;
-        const int r0 = 64 * wm + 32 * i;
+        const int r0 = T::WM * wm + 32 * i;
         if (row_sum) {
             const float t = rsum[i] + __shfl_xor(rsum[i], 32, 64);
             if (lane < 32 && r0 + lane < M)
@@ -1343,51 +1342,41 @@ struct RowSums {
     }
 };
 
-// 64 live rows a block, a lane each; the waves share the strips, four at a time.
+// LR live rows a block; of each wave 64 / LR lanes a row, which share the strips with
+// the other waves', four at a time.
+template <int LR>
 __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p) {
     // max z / T and z / T of a target are to be rounded alike: their difference counts
 #pragma clang fp contract(off)
-    constexpr int W = kFinishWaves, U = 4;
-    __shared__ float mx_s[W][64], sum_s[W][64], sumt_s[W][64], cross_s[64];
+    constexpr int W = kFinishWaves, U = 4, SHARE = 64 / LR * W;
+    __shared__ float mx_s[W][LR], sum_s[W][LR], sumt_s[W][LR], cross_s[LR];
     __shared__ double part_s[W][4];
     __shared__ bool last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int live = p.s.head->live;
-    const int r = blockIdx.x * 64 + lane;
+    const int lr = lane % LR, r = blockIdx.x * LR + lr;
     const bool in = r < live, two = p.sum_t != nullptr;
     const float scale = kLog2e * p.inv, scale_t = kLog2e * p.inv_t;
-    RowSums z;
-    // sum_j q_j z_j / T of four rows a wave, a lane an entry (z of one that is none is 0)
-    if (p.K > 0) {
-#pragma unroll
-        for (int u = 0; u < 64 / W; ++u) {
-            const int row = blockIdx.x * 64 + wave * (64 / W) + u;
-            const size_t entry = static_cast<size_t>(min(row, max(live - 1, 0))) * (1 + p.K) + 1;
-            float v = 0.0f;
-            for (int j = lane; j < p.K; j += 64)
-                v = __builtin_fmaf(p.s.tq[entry + j], p.s.tz[entry + j] * p.inv_t, v);
-            v = wave_total(v);
-            if (lane == 0) cross_s[wave * (64 / W) + u] = v;
-        }
-    }
     // (requested ahead of the strips)
+    const bool owner = wave == 0 && lane < LR && in;
     float2 weight = make_float2(0.0f, 0.0f);
     float4 rec = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float zlabel = 0.0f;
     int row = 0;
-    if (wave == 0 && in) {
+    if (owner) {
         weight = p.s.weight[r];
         rec = p.s.rec[r];
         zlabel = p.s.tz[static_cast<size_t>(r) * (1 + p.K)];
         row = p.s.row[r];
     }
+    RowSums z;
     if (in) {
-        for (int q = wave; q < p.strips; q += U * W) {
+        for (int q = wave * (64 / LR) + lane / LR; q < p.strips; q += U * SHARE) {
             float m2[U], s2[U], t2[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const bool there = q + u * W < p.strips;
-                const size_t at = static_cast<size_t>(there ? q + u * W : q) * p.N + r;
+                const bool there = q + u * SHARE < p.strips;
+                const size_t at = static_cast<size_t>(there ? q + u * SHARE : q) * p.N + r;
                 m2[u] = p.mx[at];
                 s2[u] = p.sum[at];
                 t2[u] = two ? p.sum_t[at] : 0.0f;
@@ -1396,27 +1385,45 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
             z.join<U, true>(m2, s2, t2, scale, scale_t, two);
         }
     }
-    float m = z.m, s = z.s, st = z.t;
-    mx_s[wave][lane] = m;
-    sum_s[wave][lane] = s;
-    sumt_s[wave][lane] = st;
+    // sum_j q_j z_j / T, a row a wave at a time, a lane an entry (z of one that is none
+    // is 0)
+    if (p.K > 0) {
+        for (int u = wave; u < LR; u += W) {
+            const int k = blockIdx.x * LR + u;
+            if (k >= live) break;
+            const size_t entry = static_cast<size_t>(k) * (1 + p.K) + 1;
+            float v = 0.0f;
+            for (int j = lane; j < p.K; j += 64)
+                v = __builtin_fmaf(p.s.tq[entry + j], p.s.tz[entry + j] * p.inv_t, v);
+            v = wave_total(v);
+            if (lane == 0) cross_s[u] = v;
+        }
+    }
+#pragma unroll
+    for (int o = LR; o < 64; o <<= 1) {
+        const float m2[1] = {__shfl_xor(z.m, o, 64)}, s2[1] = {__shfl_xor(z.s, o, 64)};
+        const float t2[1] = {__shfl_xor(z.t, o, 64)};
+        z.join<1, false>(m2, s2, t2, scale, scale_t, two);
+    }
+    if (lane < LR) {
+        mx_s[wave][lr] = z.m;
+        sum_s[wave][lr] = z.s;
+        sumt_s[wave][lr] = z.t;
+    }
     __syncthreads();
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
     if (wave == 0) {
-        double v[4] = {0.0, 0.0, 0.0, 0.0};
-        if (in) {
+        if (owner) {
             float m2[W - 1], s2[W - 1], t2[W - 1];
 #pragma unroll
             for (int w = 1; w < W; ++w) {
-                m2[w - 1] = mx_s[w][lane];
-                s2[w - 1] = sum_s[w][lane];
-                t2[w - 1] = sumt_s[w][lane];
+                m2[w - 1] = mx_s[w][lr];
+                s2[w - 1] = sum_s[w][lr];
+                t2[w - 1] = sumt_s[w][lr];
             }
             z.join<W - 1, false>(m2, s2, t2, scale, scale_t, two);
-            m = z.m;
-            s = z.s;
-            st = z.t;
-            if (p.sum_t == nullptr) st = s;
-            const float cross = p.K > 0 ? cross_s[lane] : 0.0f;
+            const float m = z.m, s = z.s, st = two ? z.t : z.s;
+            const float cross = p.K > 0 ? cross_s[lr] : 0.0f;
             // (a live row's weight is not 0)
             const bool label = weight.x != 0.0f, taught = weight.y != 0.0f;
             const float lse = m * p.inv + logf(s), lse_t = m * p.inv_t + logf(st);
@@ -1437,22 +1444,33 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
 #pragma unroll
-            for (int o = 32; o > 0; o >>= 1) v[c] += __shfl_xor(v[c], o, 64);
+            for (int o = LR / 2; o > 0; o >>= 1) v[c] += __shfl_xor(v[c], o, 64);
         }
-        if (lane == 0) {
-            // (agent scope: the last block may run on another XCD)
+    }
+    auto write = [&](int i, double sum, double n) {
+        if (p.mean) sum = n != 0.0 ? sum / n : 0.0;
+        p.losses[i] = static_cast<float>(sum);
+        p.losses[2 + i] = static_cast<float>(n);
+        p.s.head->sum[i] = static_cast<float>(n);
+    };
+    if (gridDim.x == 1) {
+        if (tid < 2) write(tid, tid == 0 ? v[0] : v[1], tid == 0 ? v[2] : v[3]);
+        return;
+    }
+    if (tid == 0) {
+        // (agent scope: the last block may run on another XCD)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-                __hip_atomic_store(p.sums + 4 * blockIdx.x + c, v[c], __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_AGENT);
-            last = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_ACQ_REL,
-                                          __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-        }
+        for (int c = 0; c < 4; ++c)
+            __hip_atomic_store(p.sums + 4 * blockIdx.x + c, v[c], __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
+        last = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
+               gridDim.x - 1;
     }
     __syncthreads();
     if (!last) return;
-    double v[4] = {0.0, 0.0, 0.0, 0.0};
-    const int blocks = min(static_cast<int>(gridDim.x), (live + 63) / 64);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = 0.0;
+    const int blocks = min(static_cast<int>(gridDim.x), (live + LR - 1) / LR);
     for (int q = tid; q < blocks; q += 64 * W)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -1471,10 +1489,7 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
             a += part_s[w][tid];
             n += part_s[w][2 + tid];
         }
-        if (p.mean) a = n != 0.0 ? a / n : 0.0;
-        p.losses[tid] = static_cast<float>(a);
-        p.losses[2 + tid] = static_cast<float>(n);
-        p.s.head->sum[tid] = static_cast<float>(n);
+        write(tid, a, n);
     }
 }
 
@@ -1619,7 +1634,7 @@ double ends_at(double cus, double n, double t, double n2, double t2) {
 
 // Times are in units of a 64-deep stage of a 256 x 256 tile on one CU (1.8 us): a tile
 // takes its stages, and 8 more for its start and its outputs; f32 sums that are written
-// and read again cost the memory 0.07 a 256 x 256 tile and range. Both products are one
+// and read again cost the memory 0.09 a 256 x 256 tile and range. Both products are one
 // launch, dx first.
 Cut choose_cut(const vmoe_head_shape& s, long long cols) {
     const bool f32 = s.dtype != VMOE_BF16;
@@ -1629,11 +1644,11 @@ Cut choose_cut(const vmoe_head_shape& s, long long cols) {
     Cut best{0, 1, 1};
     double least = 1e300;
     for (int narrow = 0; narrow < (f32 ? 1 : 2); ++narrow) {
-        const int bm = f32 ? 128 : 256, bn = f32 ? 128 : narrow ? 192 : 256;
-        // (a stage of 128 x 128 in f32 takes as long as two of 256 x 256 in bf16, and two
+        const int bm = f32 ? 64 : 256, bn = f32 ? 128 : narrow ? 192 : 256;
+        // (a stage of 64 x 128 in f32 takes as long as one of 256 x 256 in bf16; two such
         // blocks share a CU)
-        const double stage = f32 ? 2.0 : narrow ? 0.75 * 1.05 : 1.0, extra = f32 ? 1.0 : 8.0;
-        const double cus = f32 ? 2 * kCus : kCus, part = 0.07 * bm * bn / 65536;
+        const double stage = f32 ? 1.0 : narrow ? 0.75 * 1.05 : 1.0, extra = f32 ? 1.0 : 8.0;
+        const double cus = f32 ? 2 * kCus : kCus, part = 0.09 * bm * bn / 65536;
         const double wide = static_cast<double>((d + bn - 1) / bn);
         const double tx = static_cast<double>((N + bm - 1) / bm) * wide;
         const double tw = static_cast<double>((cols + bm - 1) / bm) * wide;
@@ -1668,7 +1683,7 @@ Plan make_plan(const vmoe_head_shape& s) {
     const long long vpad = padded_classes(s);
     long long cols = static_cast<long long>(kPieceBytes / (N * elem_bytes(s))) / 256 * 256;
     // (a piece's rows of weight stay within 32-bit offsets)
-    const long long wcols = ((1LL << 30) - 1) / d / 256 * 256;
+    const long long wcols = ((1LL << 31) / elem_bytes(s) - 1) / d / 256 * 256;
     cols = cols < wcols ? cols : wcols;
     cols = cols < 256 ? 256 : cols;
     p.pieces = static_cast<int>((vpad + cols - 1) / cols);
@@ -1692,7 +1707,7 @@ static_assert(TileBig::BN == 256 && TileBig::WGN == 2 && F32Tile::BN == 128 && F
               "two strips a tile of z");
 
 struct FwdPlan {
-    int few, row_blocks, strips, finish_blocks, two;
+    int few, row_blocks, strips, finish_rows, finish_blocks, two;
     int tile_rows, tile_shift, tiles_n;  // of z
     size_t counts_off, ticket_off, sums_off, mx_off, sum_off, sumt_off, list_off, ends_off, bytes;
 };
@@ -1706,7 +1721,9 @@ FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     p.tiles_n = static_cast<int>(cdiv(s.n_classes, 1 << p.tile_shift));
     p.few = s.n_rows <= kFewRows;
     p.strips = p.few ? static_cast<int>(cdiv(s.n_classes, kFewClasses)) : 2 * p.tiles_n;
-    p.finish_blocks = s.n_rows > 0 ? static_cast<int>(cdiv(s.n_rows, 64)) : 1;
+    // few rows: four lanes a row, since many strips stand before each
+    p.finish_rows = s.n_rows <= 1024 ? 16 : 64;
+    p.finish_blocks = s.n_rows > 0 ? static_cast<int>(cdiv(s.n_rows, p.finish_rows)) : 1;
     p.two = labels && s.n_teacher > 0 && s.temperature != 1.0f;
     Carver c{nullptr};
     auto take = [&](size_t bytes) {
@@ -1839,7 +1856,8 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
     const FinishArgs f{v, mx, sum, sum_t, reinterpret_cast<double*>(base + p.sums_off), zb.ticket,
                        losses, row_losses, p.strips, N, K, s.reduction == VMOE_REDUCE_MEAN,
                        s.temperature, inv, inv_t};
-    finish_kernel<<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
+    if (p.finish_rows == 16) finish_kernel<16><<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
+    else finish_kernel<64><<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
     return launch_status();
 }
 
@@ -1901,6 +1919,7 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
                 else subtract_kernel<float, R><<<cdiv(N, 4), 256, 0, st>>>(u);
             };
             if (s.n_teacher < 64) go(std::integral_constant<int, 1>{});
+            else if (s.n_teacher < 128) go(std::integral_constant<int, 2>{});
             else go(std::integral_constant<int, (VMOE_HEAD_MAX_TEACHER + 64) / 64>{});
         }
         PartArgs<true> l{};
