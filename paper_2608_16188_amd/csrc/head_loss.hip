@@ -178,14 +178,119 @@ struct PartArgs : Product {
 struct StoreArgs : Product {  // dz^T times x, rounded, k in one range
     void* c;      // [M, N], or null
     void* sums;   // [M] of A's rows, or null
+    const Header* head;
+    float w_label, w_teacher;
+    int mean;
     static constexpr int OUT = EPI_F32;
     static constexpr bool A_KMAJOR = false, B_KMAJOR = false;
 };
 
+// ------------------------------------------------------------------ dz of a row
+
+// What both losses' gradients are scaled by, apart from the rows' weights: g and h of
+// vmoe_head_loss_bwd. dz is formed without the larger of the two (all), which its
+// products are multiplied by instead: a label's p - 1 is near -1 then, where bf16 is
+// finest, while w / sum may stand at the start of a binade, where it is coarsest.
+struct Rates {
+    float label, teacher, all;
+    __device__ __forceinline__ Rates(const Header& h, float w_label, float w_teacher, int mean)
+        : label(w_label), teacher(w_teacher) {
+        if (mean) {
+            label = h.sum[0] != 0.0f ? label / h.sum[0] : 0.0f;
+            teacher = h.sum[1] != 0.0f ? teacher / h.sum[1] : 0.0f;
+        }
+        all = fmaxf(fabsf(label), fabsf(teacher));
+        if (all > 0.0f) {
+            label /= all;
+            teacher /= all;
+        }
+    }
+    __device__ __forceinline__ float2 of(const float2& weight) const {
+        return make_float2(label * weight.x, teacher * weight.y);
+    }
+};
+
+// One softmax or two at logit z of a row, times their weights g: see Saved::rec.
+struct Softmax {
+    bool two;
+    float scale, scale_t;
+    __device__ __forceinline__ Softmax(const Header& h, int teacher, float inv_t)
+        : two(teacher && h.labelled && inv_t != 1.0f),
+          scale(kLog2e * (teacher && !h.labelled ? inv_t : 1.0f)), scale_t(kLog2e * inv_t) {}
+    template <bool TWO>
+    __device__ __forceinline__ float at(float z, const float4& rec, const float2& g) const {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z - rec.x, scale, -rec.y));
+        if constexpr (!TWO) return (g.x + g.y) * p;
+        const float pt = __builtin_amdgcn_exp2f(__builtin_fmaf(z - rec.x, scale_t, -rec.z));
+        return __builtin_fmaf(g.x, p, g.y * pt);
+    }
+};
+
+// ------------------------------------------------------------------ tiles
+
+// What an epilogue needs of its rows, requested before the products (behind them, its
+// latency would stand alone: dz of 6304 x 768 against 32003 classes 340 -> 335 us).
+template <class T, class ARGS>
+struct Ahead {
+    __device__ __forceinline__ void load(const ARGS&, int, int, int) {}
+};
+
 // The tile that finish_tile is called for.
-template <class ARGS>
+template <class T, class ARGS>
 struct Tiled : ARGS {
     int t_m0, t_n0, t_n, t_split;  // first row and column, number of the column of tiles
+    Ahead<T, ARGS> ahead;
+};
+
+// The row of block i of the wave's rows in a tile of which M rows are left.
+template <class T>
+__device__ __forceinline__ int lane_row(int i, int M) {
+    const int wm = wave_id() / T::WGN, lane = threadIdx.x & 31;
+    return min(T::WM * wm + 32 * i + lane, M - 1);
+}
+
+template <class T>
+struct Ahead<T, StatsArgs> {
+    int label[T::FM], from, to;
+    __device__ __forceinline__ void load(const StatsArgs& p, int m0, int tn, int M) {
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+            label[i] = p.tidx[static_cast<size_t>(m0 + lane_row<T>(i, M)) * p.per_row];
+        from = to = 0;
+        if (p.list != nullptr) {
+            const size_t tile = static_cast<size_t>(m0 / T::BM) * p.tiles_n + tn;
+            to = p.ends[tile];
+            from = tn > 0 ? p.ends[tile - 1] : 0;
+        }
+    }
+};
+
+template <class T>
+struct Ahead<T, GradZArgs> {
+    Header h;
+    float4 rec[T::FM];
+    float2 weight[T::FM];
+    int label[T::FM];
+    __device__ __forceinline__ void load(const GradZArgs& p, int m0, int, int M) {
+        h = *p.head;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const int r = m0 + lane_row<T>(i, M);
+            rec[i] = p.rec[r];
+            weight[i] = p.weight[r];
+            label[i] = p.label != nullptr ? p.label[r] : -1;
+        }
+    }
+};
+
+template <class T>
+struct Ahead<T, StoreArgs> {
+    float all;
+    __device__ __forceinline__ void load(const StoreArgs& p, int, int, int) {
+        const float f = Rates(*p.head, p.w_label, p.w_teacher, p.mean).all;
+        all = __builtin_bit_cast(
+            float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
+    }
 };
 
 // Block b runs on XCD b mod 8; XCDs take chunks of neighbouring tiles in turn, and
@@ -219,7 +324,7 @@ __device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const fl
 // One tile: the operands are taken from the tile's corner and its range of k on, so that
 // offsets inside it fit 32 bits however large they are.
 template <class T, class ARGS>
-__device__ __forceinline__ bool place_tile(const ARGS& args, int block, Tiled<ARGS>* p,
+__device__ __forceinline__ bool place_tile(const ARGS& args, int block, Tiled<T, ARGS>* p,
                                            const Elm<T>** a, const Elm<T>** b, int* M, int* N,
                                            int* K) {
     constexpr bool A_KMAJOR = ARGS::A_KMAJOR, B_KMAJOR = ARGS::B_KMAJOR;
@@ -254,10 +359,11 @@ template <class T, class ARGS>
 __device__ __forceinline__ void run_tile(const ARGS& args, int block, uint16_t* a0, uint16_t* a1,
                                          uint16_t* bl0, uint16_t* bh0, uint16_t* bl1,
                                          uint16_t* bh1, uint16_t* stg) {
-    Tiled<ARGS> p;
+    Tiled<T, ARGS> p;
     const Elm<T>*a, *b;
     int M, N, K;
     if (!place_tile<T>(args, block, &p, &a, &b, &M, &N, &K)) return;
+    p.ahead.load(args, p.t_m0, p.t_n, M);
     if constexpr (is_f32<T>()) {
         f32_tile<T>(p, a, b, M, N, K, reinterpret_cast<float*>(a0), reinterpret_cast<float*>(a1));
     } else {
@@ -516,7 +622,7 @@ __device__ __forceinline__ void store_block(const f32x16& v, lds_u16* s, E* dst,
 // right to the last digit). Bound by the vector unit beside the matrix instructions: an
 // exponential is four slots, the rest 2.5.
 template <class T, int EPI>
-__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsArgs>& p,
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, StatsArgs>& p,
                                             f32x16 (&acc)[T::FM][T::PB], float (&)[T::FM], bool,
                                             const LdsArrays& arrays, int, int M, int N, int, int,
                                             int fm_live) {
@@ -528,7 +634,7 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsA
         if (i >= fm_live) break;
         const int r0 = T::WM * wm + 32 * i;
         const size_t row = p.t_m0 + min(r0 + (lane & 31), M - 1);
-        const int spot = class_spot<T>(p.tidx[row * p.per_row], p.t_n0);
+        const int spot = class_spot<T>(p.ahead.label[i], p.t_n0);
         float m = kLowest;
 #pragma unroll
         for (int b = 0; b < T::PB; ++b)
@@ -569,8 +675,7 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsA
     if (p.list == nullptr) return;
     // The logits of the tile's entries: a lane an entry, 32 x 32 blocks with one of
     // them through LDS.
-    const size_t tile = static_cast<size_t>(p.t_m0 / T::BM) * p.tiles_n + p.t_n;
-    const int to = p.ends[tile], from = p.t_n > 0 ? p.ends[tile - 1] : 0;
+    const int from = p.ahead.from, to = p.ahead.to;
     const uint32_t* const list = p.list + static_cast<size_t>(p.t_m0) * (p.per_row - 1);
     lds_u16* const s = wave_lds(arrays);
     for (int e0 = from; e0 < to; e0 += 64) {
@@ -595,57 +700,32 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StatsA
     }
 }
 
-// Weights of the two softmaxes in a row's dz.
-__device__ __forceinline__ float2 row_rates(const Header& h, const float2& weight, float w_label,
-                                            float w_teacher, int mean) {
-    float g = w_label * weight.x, t = w_teacher * weight.y;
-    if (mean) {
-        g = h.sum[0] != 0.0f ? g / h.sum[0] : 0.0f;
-        t = h.sum[1] != 0.0f ? t / h.sum[1] : 0.0f;
-    }
-    return make_float2(g, t);
-}
-
-// One softmax or two at logit z of a row, times their weights g: see Saved::rec.
-struct Softmax {
-    bool two;
-    float scale, scale_t;
-    __device__ __forceinline__ Softmax(const Header& h, int teacher, float inv_t)
-        : two(teacher && h.labelled && inv_t != 1.0f),
-          scale(kLog2e * (teacher && !h.labelled ? inv_t : 1.0f)), scale_t(kLog2e * inv_t) {}
-    template <bool TWO>
-    __device__ __forceinline__ float at(float z, const float4& rec, const float2& g) const {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z - rec.x, scale, -rec.y));
-        if constexpr (!TWO) return (g.x + g.y) * p;
-        const float pt = __builtin_amdgcn_exp2f(__builtin_fmaf(z - rec.x, scale_t, -rec.z));
-        return __builtin_fmaf(g.x, p, g.y * pt);
-    }
-};
-
 // dz, but for a teacher's targets. One softmax serves both losses where the temperature
 // is 1 or only one of them is there. bf16: the weight goes into the exponent, a
 // row's sign into the rounded values, and lse into one constant, whose rounding moves
 // p by some 2^-24 |log2|, far below the rounding of dz; f32 keeps z - max z and the
 // logarithm of the sum apart.
 template <class T, int EPI>
-__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<GradZArgs>& p,
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, GradZArgs>& p,
                                             f32x16 (&acc)[T::FM][T::PB], float (&)[T::FM], bool,
                                             const LdsArrays& arrays, int, int M, int N, int, int,
                                             int fm_live) {
     constexpr bool F32 = is_f32<T>();
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int wm = wave / T::WGN, wn = wave % T::WGN;
-    const Header h = *p.head;
+    const Header& h = p.ahead.h;
     const Softmax soft(h, p.teacher, p.inv_t);
+    const Rates rates(h, p.w_label, p.w_teacher, p.mean);
     if (h.biased || N < T::BN) add_bias<T>(acc, p.zbias, p.t_n0);
     Elm<T>* const dz = static_cast<Elm<T>*>(p.dz);
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         if (i >= fm_live) break;
-        const int r0 = T::WM * wm + 32 * i, r = p.t_m0 + min(r0 + (lane & 31), M - 1);
-        const float4 rec = p.rec[r];
-        const float2 g = row_rates(h, p.weight[r], p.w_label, p.w_teacher, p.mean);
-        const int spot = p.label != nullptr ? class_spot<T>(p.label[r] - p.first, p.t_n0) : -1;
+        const int r0 = T::WM * wm + 32 * i;
+        const float4 rec = p.ahead.rec[i];
+        const float2 g = rates.of(p.ahead.weight[i]);
+        const int label = p.ahead.label[i];
+        const int spot = label >= 0 ? class_spot<T>(label - p.first, p.t_n0) : -1;
         const bool any = __any(spot >= 0);
         const float all = g.x + g.y;
         const bool down = !F32 && !soft.two && all < 0.0f;
@@ -694,7 +774,7 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<GradZA
 
 // f32 sums of the tile's range of k, into its slot.
 template <class T, int EPI, bool LEFT>
-__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<PartArgs<LEFT>>& p,
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, PartArgs<LEFT>>& p,
                                             f32x16 (&acc)[T::FM][T::PB], float (&rsum)[T::FM],
                                             bool row_sum, const LdsArrays& arrays, int, int M,
                                             int N, int, int, int fm_live) {
@@ -738,13 +818,14 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<PartAr
 
 // The product rounded to its type.
 template <class T, int EPI>
-__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StoreArgs>& p,
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, StoreArgs>& p,
                                             f32x16 (&acc)[T::FM][T::PB], float (&rsum)[T::FM],
                                             bool row_sum, const LdsArrays& arrays, int, int M,
                                             int N, int, int, int fm_live) {
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int wm = wave / T::WGN, wn = wave % T::WGN;
     Elm<T>* const c = static_cast<Elm<T>*>(p.c);
+    const float all = p.ahead.all;
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         if (i >= fm_live) break;
@@ -752,14 +833,17 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<StoreA
         if (row_sum) {
             const float t = rsum[i] + __shfl_xor(rsum[i], 32, 64);
             if (lane < 32 && r0 + lane < M)
-                Elem<Elm<T>>::store(static_cast<Elm<T>*>(p.sums), p.t_m0 + r0 + lane, t);
+                Elem<Elm<T>>::store(static_cast<Elm<T>*>(p.sums), p.t_m0 + r0 + lane, t * all);
         }
         if (c == nullptr) continue;
 #pragma unroll
         for (int b = 0; b < T::PB; ++b) {
             const int n = 64 * b + 32 * wn;
             if (n >= N) break;
-            store_block(acc[i][b], wave_lds(arrays),
+            f32x16 v = acc[i][b];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) v[q] *= all;
+            store_block(v, wave_lds(arrays),
                         c + static_cast<size_t>(p.t_m0 + r0) * p.N + p.t_n0 + n, p.N, M - r0,
                         N - n);
         }
@@ -1286,7 +1370,7 @@ __global__ __launch_bounds__(256) void few_grad_kernel(FewGradArgs p) {
     const int r = tid >> 2, c0 = 8 * (tid & 3);
     if (r >= h.live) return;
     const float4 rec = p.s.rec[r];
-    const float2 g = row_rates(h, p.s.weight[r], p.w_label, p.w_teacher, p.mean);
+    const float2 g = Rates(h, p.w_label, p.w_teacher, p.mean).of(p.s.weight[r]);
     const Softmax soft(h, p.K > 0, p.inv_t);
     // (with a teacher, subtract_kernel sees to the targets)
     const int label = p.K == 0 ? p.s.tidx[r] - p.first - n0 - c0 : -1;
@@ -1512,7 +1596,7 @@ __global__ __launch_bounds__(256) void subtract_kernel(SubtractArgs p) {
     const int n = 1 + p.K;
     const size_t at = static_cast<size_t>(r) * n;
     const float4 rec = p.s.rec[r];
-    const float2 g = row_rates(h, p.s.weight[r], p.w_label, p.w_teacher, p.mean);
+    const float2 g = Rates(h, p.w_label, p.w_teacher, p.mean).of(p.s.weight[r]);
     const Softmax soft(h, p.teacher, p.inv_t);
     int idx[R];
     float share[R], z[R], hit[R];
@@ -1546,13 +1630,23 @@ __global__ __launch_bounds__(256) void subtract_kernel(SubtractArgs p) {
     }
 }
 
+// The factor that dz was formed without, for the kernels below.
+struct Factor {
+    const Header* head;
+    float w_label, w_teacher;
+    int mean;
+    __device__ __forceinline__ float get() const {
+        return Rates(*head, w_label, w_teacher, mean).all;
+    }
+};
+
 // dx: the slots' sums, rounded, to the rows' places; zeros for rows left out. Eight
 // columns a thread, the slots shared by G of them (many slots stand before few rows,
 // whose threads alone would wait for one after the other).
 template <typename E, int G>
 __global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ part, size_t stride,
                                                  int slots, const int32_t* __restrict__ place,
-                                                 E* __restrict__ dx, int N, int d) {
+                                                 E* __restrict__ dx, int N, int d, Factor factor) {
     constexpr int PER = 256 / G;
     __shared__ float sum_s[G > 1 ? G : 1][G > 1 ? PER : 1][8];
     const int per = d / 8, of = threadIdx.x % PER, g = threadIdx.x / PER;
@@ -1581,6 +1675,9 @@ __global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ part,
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] += sum_s[k][of][q];
     }
+    const float all = factor.get();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= all;
     if (in) store8(dx + static_cast<size_t>(t) * d + c, v);
 }
 
@@ -1589,13 +1686,14 @@ template <typename E>
 __global__ __launch_bounds__(256) void dw_kernel(const float* __restrict__ part, size_t stride,
                                                  const float* __restrict__ part_sums, int slots,
                                                  E* __restrict__ dw, E* __restrict__ db, int M,
-                                                 int d) {
+                                                 int d, Factor factor) {
     const int per = d / 8;
     const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    const float all = factor.get();
     if (db != nullptr && i < M) {
         float v = 0.0f;
         for (int s = 0; s < slots; ++s) v += part_sums[static_cast<size_t>(s) * M + i];
-        Elem<E>::store(db, i, v);
+        Elem<E>::store(db, i, v * all);
     }
     if (i >= static_cast<long long>(M) * per) return;
     float v[8] = {};
@@ -1606,6 +1704,8 @@ __global__ __launch_bounds__(256) void dw_kernel(const float* __restrict__ part,
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] += w[q];
     }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= all;
     store8(dw + 8 * i, v);
 }
 
@@ -1870,6 +1970,8 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
     const int N = s.n_rows, V = s.n_classes, d = s.d_model;
     const size_t size = elem_bytes(s);
     const bool bf16 = s.dtype == VMOE_BF16;
+    const Factor factor{v.head, w_label, w_teacher * s.temperature,
+                        s.reduction == VMOE_REDUCE_MEAN};
     for (int i = 0; i < p.pieces; ++i) {
         const int first = i * p.cols, count = min(p.cols, V - first);
         if (count <= 0) break;
@@ -1889,10 +1991,10 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
         z.weight = v.weight;
         z.dz = base + p.dz_off;
         z.ldz = static_cast<int>(up256(count));
-        z.w_label = w_label;
-        z.w_teacher = w_teacher * s.temperature;
+        z.w_label = factor.w_label;
+        z.w_teacher = factor.w_teacher;
         z.inv_t = 1.0f / s.temperature;
-        z.mean = s.reduction == VMOE_REDUCE_MEAN;
+        z.mean = factor.mean;
         z.teacher = s.n_teacher > 0;
         z.label = z.teacher ? nullptr : v.tidx;
         z.first = first;
@@ -1957,6 +2059,10 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             c.c = dwp;
             c.sums = dbp;
             c.bsum = reinterpret_cast<float*>(dbp);
+            c.head = v.head;
+            c.w_label = factor.w_label;
+            c.w_teacher = factor.w_teacher;
+            c.mean = factor.mean;
             launch_products(s, p.cut.narrow, l, rows_l, c, rows_r, st);
         } else {
             PartArgs<false> c{};
@@ -1970,11 +2076,11 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             if (bf16)
                 dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, r.splits,
                                                 reinterpret_cast<uint16_t*>(dwp),
-                                                reinterpret_cast<uint16_t*>(dbp), count, d);
+                                                reinterpret_cast<uint16_t*>(dbp), count, d, factor);
             else
                 dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, r.splits,
                                                 reinterpret_cast<float*>(dwp),
-                                                reinterpret_cast<float*>(dbp), count, d);
+                                                reinterpret_cast<float*>(dbp), count, d, factor);
         }
     }
     if (dx != nullptr && N > 0) {
@@ -1985,10 +2091,10 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             const unsigned grid = cdiv(static_cast<long long>(N) * (d / 8), 256 / G);
             if (bf16)
                 dx_kernel<uint16_t, G><<<grid, 256, 0, st>>>(part, stride, p.cut.dx, v.place,
-                                                             static_cast<uint16_t*>(dx), N, d);
+                                                             static_cast<uint16_t*>(dx), N, d, factor);
             else
                 dx_kernel<float, G><<<grid, 256, 0, st>>>(part, stride, p.cut.dx, v.place,
-                                                          static_cast<float*>(dx), N, d);
+                                                          static_cast<float*>(dx), N, d, factor);
         };
         if (p.cut.dx >= 16) go(std::integral_constant<int, 8>{});
         else go(std::integral_constant<int, 1>{});
