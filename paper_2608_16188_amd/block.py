@@ -2,13 +2,15 @@
 
     h     = norm(x)                                   before the layer
     x_out = x + row_scale gate post(layer(h)),  h_out = norm(x_out)
-    loss  = the caller's on h_out and x_out, plus the gate's balance and z losses
+    loss  = the caller's on h_out and x_out, plus the gate's balance and z losses;
+            with a head over classes, its label and teacher losses on h_out
 
 `SparseBlock` owns the stream, the norms' and the gate's parameters and their
 gradients beside the layer's `LayerBuffers`, all allocated once; `forward`,
 `backward` and `update` enqueue their calls on the current stream and allocate
 nothing; `update` also waits for the update before it, to learn whether that one
-was skipped. `python -m paper_2608_16188_amd.block` trains one on a fixed target.
+was skipped. `python -m paper_2608_16188_amd.block` trains one on a fixed target, or
+with `--classes` on labels and a teacher's best classes.
 """
 from __future__ import annotations
 
@@ -19,6 +21,7 @@ import time
 
 import torch
 
+from . import vmoe_head as H
 from . import vmoe_train as T
 from . import workloads as W
 from .layer import LayerBuffers
@@ -41,28 +44,37 @@ class SparseBlock:
     def __init__(self, cfg: W.LayerConfig, inputs: dict, *, norm: str = "layer",
                  post_norm: str = "none", gate_init: float = 0.1, row_scale: bool = False,
                  w_balance: float = 0.01, w_z: float = 0.001, state_bits: int = 32,
-                 weight_decay: float = 0.05, max_norm: float = 1.0, device="cuda"):
+                 weight_decay: float = 0.05, max_norm: float = 1.0, classes: int = 0,
+                 teacher_top: int = 0, temperature: float = 1.0, w_label: float = 1.0,
+                 w_teacher: float = 1.0, device="cuda"):
         """norm: rms or layer, of the layer's input and of x_out; post_norm: none,
         rms or layer, of the layer's output. row_scale: whether tokens have a scale
         for the layer's output (drop-path; `self.row_scale`, ones at first).
         state_bits: 32, or 8 to keep AdamW's moments of tensors of 16384 elements or
-        more in 8 bits. The tokens in `inputs` are the stream's first content."""
+        more in 8 bits. The tokens in `inputs` are the stream's first content.
+        classes: of a head on h_out (0: none), which learns from labels and, with
+        teacher_top, from a teacher's lists of that many classes."""
         for name, value, allowed in (("norm", norm, ("rms", "layer")),
                                      ("post_norm", post_norm, ("none", "rms", "layer")),
                                      ("state_bits", state_bits, (8, 32))):
             if value not in allowed:
                 raise ValueError(f"{name}: one of {allowed} is wanted, got {value!r}")
+        if classes < 0 or not 0 <= teacher_top <= (H.MAX_TEACHER if classes else 0):
+            raise ValueError(f"classes, teacher_top: a head of 0 classes has no teacher, others a "
+                             f"list of up to {H.MAX_TEACHER}, got {classes}, {teacher_top}")
         self.layer = L = LayerBuffers(cfg, inputs, device)
         self.w_balance, self.w_z, self.max_norm = w_balance, w_z, max_norm
         N, G, d, E = max(cfg.n_tokens, 1), cfg.n_groups, cfg.d_model, cfg.n_experts
         act, f32, dev = L.x.dtype, torch.float32, L.device
         dt = L.shape.dtype
 
-        def shape(post):
+        def shape(post, dh):
             return T.make_norm_shape(cfg.n_tokens, d, dt, pre_norm=NORMS[norm],
-                                     post_norm=NORMS[post])
+                                     post_norm=NORMS[post], dh_dtype=dh)
 
-        self.in_shape, self.out_shape = shape("none"), shape(post_norm)
+        self.in_shape = shape("none", T.VMOE_F32)
+        # (a head hands its gradient over in the activations' type)
+        self.out_shape = shape(post_norm, dt if classes else T.VMOE_F32)
         new = lambda dtype, *s: torch.empty(*s, dtype=dtype, device=dev)  # noqa: E731
         self.x = L.x.clone()  # the stream; the layer's x becomes its norm
         self.x_out, self.h_out = new(act, N, d), new(act, N, d)
@@ -80,6 +92,23 @@ class SparseBlock:
         if post_norm == "layer":
             self.params["post_b"] = torch.zeros(d, dtype=act, device=dev)
         self.grads = {k: new(f32, d) for k in self.params}
+        self.head_shape = None
+        if classes:
+            self.head_shape = hs = H.make_head_shape(cfg.n_tokens, d, classes, dt,
+                                                     n_teacher=teacher_top,
+                                                     temperature=temperature)
+            self.w_label, self.w_teacher = w_label, w_teacher
+            gen = torch.Generator(device=dev).manual_seed(0)
+            self.params["head_w"] = (0.02 * torch.randn(classes, d, device=dev,
+                                                        generator=gen)).to(act)
+            self.params["head_b"] = torch.zeros(classes, dtype=act, device=dev)
+            self.grads["head_w"], self.grads["head_b"] = new(act, classes, d), new(act, classes)
+            self.head_losses, self.row_losses = new(f32, 4), new(f32, N, 2)
+            self.dh_out = new(act, N, d)
+            self.head_saved, self.head_fwd_ws, self.head_bwd_ws = (
+                new(torch.uint8, max(f(hs), 16)) for f in (
+                    H.vmoe_head_loss_saved_bytes, H.vmoe_head_loss_fwd_workspace_bytes,
+                    H.vmoe_head_loss_bwd_workspace_bytes))
         for k in ("w1", "b1", "w2", "b2"):
             self.params[k], self.grads[k] = getattr(L, k), getattr(L, "d" + k)
         if L.dw_router is not None:
@@ -99,7 +128,8 @@ class SparseBlock:
             self.states[k] = T.adamw_state(p, bits)
         self.plan = T.AdamWPlan([
             T.AdamWTensor(param=p, grad=self.grads[k], **self.states[k],
-                          weight_decay=weight_decay if k in ("w1", "w2", "w_router") else 0.0)
+                          weight_decay=weight_decay if k in ("w1", "w2", "w_router", "head_w")
+                          else 0.0)
             for k, p in self.params.items()], dev)
         self.clip = new(f32, 2)
         self.clip_ws = ws(T.vmoe_grad_norm_workspace_bytes(self.plan))
@@ -131,9 +161,28 @@ class SparseBlock:
                               p["gate"], self.row_scale, p["out_w"], p.get("out_b"), self.x_out,
                               self.h_out, self.post_stats, self.out_stats, stream)
 
+    def head_forward(self, labels, teacher_idx=None, teacher_logits=None, row_weight=None,
+                     stream=None):
+        """The head's losses on h_out into self.head_losses (label, teacher, and the
+        rows' weights they are means over) and self.row_losses: see
+        vmoe_head_loss_fwd. A label outside the classes (-1) is none."""
+        p = self.params
+        H.vmoe_head_loss_fwd(self.head_shape, self.h_out, p["head_w"], p["head_b"], labels,
+                             teacher_idx, teacher_logits, row_weight, self.head_losses,
+                             self.row_losses, self.head_saved, self.head_fwd_ws, stream)
+
+    def head_backward(self, stream=None):
+        """Of the last head_forward: the head's gradients, then the block's."""
+        g = self.grads
+        H.vmoe_head_loss_bwd(self.head_shape, self.params["head_w"], self.head_saved,
+                             self.w_label, self.w_teacher, self.dh_out, g["head_w"], g["head_b"],
+                             self.head_bwd_ws, stream)
+        self.backward(self.dh_out, stream=stream)
+
     def backward(self, dh_out, dx_out=None, stream=None):
-        """From the loss's gradients at h_out (f32) and, along the stream, at
-        x_out (the stream's type, or None for 0) to self.grads and self.dx."""
+        """From the loss's gradients at h_out (f32; with a head, the activations'
+        type) and, along the stream, at x_out (the stream's type, or None for 0) to
+        self.grads and self.dx."""
         L, p, g = self.layer, self.params, self.grads
         T.vmoe_block_norm_bwd(self.out_shape, dx_out, dh_out, self.x_out, L.y, p.get("post_w"),
                               p.get("post_b"), p["gate"], self.row_scale, p["out_w"],
@@ -183,17 +232,49 @@ def train(cfg, inputs, target, steps, lr, report=None, **options):
     return block, torch.stack(losses).tolist()
 
 
+def train_head(cfg, inputs, labels, steps, lr, report=None, teacher=(None, None), **options):
+    """Trains a block with a head on `labels` and a teacher's (classes, logits);
+    returns the block and the objective of every step."""
+    block = SparseBlock(cfg, inputs, **options)
+    weights = torch.tensor([block.w_label, block.w_teacher], device=block.head_losses.device)
+    losses = []
+    for k in range(steps):
+        block.forward()
+        block.head_forward(labels, *teacher)
+        losses.append((block.head_losses[:2] * weights).sum())
+        block.head_backward()
+        block.update(lr * (0.55 + 0.45 * math.cos(math.pi * k / steps)), seed=1)
+        if report:
+            report(k, losses[-1], block)
+    return block, torch.stack(losses).tolist()
+
+
+def linear_teacher(x, classes, top, seed=0):
+    """Labels, and the `top` best classes and their logits, of a random linear head
+    on the tokens."""
+    gen = torch.Generator(device=x.device).manual_seed(seed)
+    weight = torch.randn(classes, x.shape[1], device=x.device, generator=gen)
+    logits = torch.matmul(x.float(), weight.T) * (3 / math.sqrt(x.shape[1]))
+    best, idx = logits.topk(max(top, 1), 1)
+    labels = idx[:, 0].to(torch.int32)
+    return labels, ((idx.to(torch.int32), best) if top else (None, None))
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--workload", choices=list(W.CONFIGS), default="vitb16_bf16")
     ap.add_argument("--steps", type=int, default=50)
     ap.add_argument("--lr", type=float, default=2e-3)
     ap.add_argument("--state-bits", type=int, choices=(8, 32), default=8)
+    ap.add_argument("--classes", type=int, default=0, help="train a head over so many classes")
+    ap.add_argument("--teacher-top", type=int, default=0,
+                    help="classes of a teacher's list for each token (with --classes)")
+    ap.add_argument("--temperature", type=float, default=2.0, help="of the distillation")
     a = ap.parse_args()
     cfg = W.CONFIGS[a.workload]
     inputs = W.make_inputs(cfg)
+    options = dict(state_bits=a.state_bits, row_scale=False)
     gen = torch.Generator(device="cuda").manual_seed(0)
-    target = torch.randn(cfg.n_tokens, cfg.d_model, device="cuda", generator=gen)
 
     def report(k, loss, block):
         if k % 10 == 0 or k == a.steps - 1:
@@ -201,7 +282,14 @@ def main():
                   f"  gradient norm {float(block.clip[0]):.3g}", flush=True)
 
     start = time.perf_counter()
-    train(cfg, inputs, target, a.steps, a.lr, report, state_bits=a.state_bits, row_scale=False)
+    if a.classes:
+        x = torch.from_numpy(W.to_f64(inputs["x"], cfg.dtype)).float().cuda()
+        labels, teacher = linear_teacher(x, a.classes, a.teacher_top)
+        train_head(cfg, inputs, labels, a.steps, a.lr, report, teacher, classes=a.classes,
+                   teacher_top=a.teacher_top, temperature=a.temperature, **options)
+    else:
+        target = torch.randn(cfg.n_tokens, cfg.d_model, device="cuda", generator=gen)
+        train(cfg, inputs, target, a.steps, a.lr, report, **options)
     torch.cuda.synchronize()
     print(f"{a.workload}: {a.steps} steps in {time.perf_counter() - start:.2f} s")
 
