@@ -37,13 +37,14 @@ typedef struct vmoe_head_shape {
 } vmoe_head_shape;
 
 /* Bytes of `saved` and of the calls' scratch (0 on an invalid shape). Neither
- * grows with N V: the logits are formed a tile at a time and never stored, their
- * gradient a piece of the classes at a time, within 1 GiB of the workspace. */
+ * grows with N V, but for at most 64 rows, whose logits `saved` holds: those of more
+ * rows are formed a tile at a time and never stored, and their gradient a piece of the
+ * classes at a time, within 1 GiB of the workspace. */
 size_t vmoe_head_loss_saved_bytes(const vmoe_head_shape* shape);
 size_t vmoe_head_loss_fwd_workspace_bytes(const vmoe_head_shape* shape);
 size_t vmoe_head_loss_bwd_workspace_bytes(const vmoe_head_shape* shape);
 
-/* The losses of a head over rows of x, z = x weight^T + bias [N, V] (not stored):
+/* The losses of a head over rows of x, z = x weight^T + bias [N, V]:
  *   label loss of row t, where labels[t] lies in [0, V):
  *     a_t = lse(z_t) - z_t[labels[t]],  lse(z) = log sum_c exp z[c]
  *   teacher loss of row t, over the entries j whose teacher_idx[t,j] = c_j lies in
@@ -82,8 +83,9 @@ vmoe_status vmoe_head_loss_fwd(const vmoe_head_shape* shape, const void* x, cons
  *   dx = dz weight [N, d] (0 for rows that were left out),
  *   dweight = dz^T x [V, d], dbias = sum_t dz [V]               dtype, overwritten
  * Each of them may be NULL and is not formed then (a frozen head, or a head alone).
- * The logits are formed again. bf16: dz is rounded to bf16 for the products, as every
- * operand of theirs is; they and the sums accumulate in f32 and are rounded once.
+ * The logits of more than 64 rows are formed again. bf16: dz is rounded to bf16 for the
+ * products, as every operand of theirs is; they and the sums accumulate in f32 and are
+ * rounded once.
  * `saved` is read only: several backwards may follow one forward. */
 vmoe_status vmoe_head_loss_bwd(const vmoe_head_shape* shape, const void* weight,
                                const void* saved, float w_label, float w_teacher, void* dx,

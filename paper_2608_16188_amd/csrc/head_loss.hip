@@ -1,11 +1,12 @@
 // A head over many classes with its losses (vmoe_head.h) on gfx950.
 //
-// z = x W^T + b is never stored. The forward forms it a tile at a time and keeps of
-// each row and strip of columns the largest value and the sum of exponentials; the
-// backward forms it again, turns it into dz a piece of the classes at a time and
-// multiplies that piece by W and by x:
+// z = x W^T + b of more than 64 rows is never stored. The forward forms it a tile at a
+// time and keeps of each row and strip of columns the largest value and the sum of
+// exponentials; the backward forms it again, turns it into dz a piece of the classes at
+// a time and multiplies that piece by W and by x (the kernels of at most 64 rows keep z,
+// V times 256 bytes at most, and read it back):
 //   mark      which rows have a label or a teacher, their places among those
-//             (1024 rows a block); the bias in f32, -infinity past the classes
+//             (256 or 1024 rows a block); the bias in f32, -infinity past the classes
 //   rows      a wave a row: the row's x to its place, its label and its teacher's
 //             entries with their q
 //   sort      with a teacher, the entries by the tile of z that they lie in
@@ -33,7 +34,6 @@ namespace vmoe {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kMarkRows = 1024;
 constexpr int kCus = 256;
 constexpr size_t kPieceBytes = size_t(1) << 30;  // dz of one piece of the classes
 // Stands for the maximum of a strip without a class: its -infinities give sums of 0
@@ -66,8 +66,12 @@ struct Saved {
     float* tz;       // [N, 1 + K] their logits
     float* tq;       // [N, 1 + K] 1 and q
     void* x;         // [N, d]
+    float* z;        // [N, V up to 256] of few rows
     size_t bytes;
 };
+
+// At most so many rows take the kernels of few rows.
+constexpr int kFewRows = 64, kFewClasses = 32;
 
 int padded_classes(const vmoe_head_shape& s) { return static_cast<int>(up256(s.n_classes)); }
 size_t elem_bytes(const vmoe_head_shape& s) { return s.dtype == VMOE_BF16 ? 2 : 4; }
@@ -97,6 +101,7 @@ Saved saved_layout(const vmoe_head_shape& s, void* base) {
     v.tz = c.take<float>(E);
     v.tq = c.take<float>(E);
     v.x = c.take<char>(N * s.d_model * elem_bytes(s));
+    v.z = c.take<float>(N <= kFewRows ? N * padded_classes(s) : 0);
     v.bytes = c.off;
     return v;
 }
@@ -524,7 +529,7 @@ __device__ __forceinline__ void f32_tile(const ARGS& p, const float* a, const fl
 
 // ------------------------------------------------------------------ tiles' outputs
 
-// Register 4 q + r of lane l, block i, panel b: row 64 wm + 32 i + l % 32, column
+// Register 4 q + r of lane l, block i, panel b: row WM wm + 32 i + l % 32, column
 // 64 b + 32 wn + 8 q + 4 (l / 32) + r of the tile.
 
 // z = product + bias in the accumulators; -infinity past the classes.
@@ -941,14 +946,14 @@ struct MarkArgs {
 };
 
 // Blocks [0, row_blocks): a row a thread; the others the bias.
-__global__ __launch_bounds__(kMarkRows) void mark_kernel(MarkArgs p) {
+__global__ __launch_bounds__(1024) void mark_kernel(MarkArgs p) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
-        pad_bias(p.bias, (blockIdx.x - p.row_blocks) * kMarkRows + tid);
+        pad_bias(p.bias, (blockIdx.x - p.row_blocks) * blockDim.x + tid);
         return;
     }
-    __shared__ int wsum[kMarkRows / 64];
-    const int t = blockIdx.x * kMarkRows + tid;
+    __shared__ int wsum[16];
+    const int t = blockIdx.x * blockDim.x + tid;
     const bool live = row_is_live(p.told, t - lane);
     const uint64_t all = __ballot(live);
     if (lane == 0) wsum[wave] = __popcll(all);
@@ -960,7 +965,7 @@ __global__ __launch_bounds__(kMarkRows) void mark_kernel(MarkArgs p) {
         if (!live && p.row_losses != nullptr)
             reinterpret_cast<float2*>(p.row_losses)[t] = make_float2(0.0f, 0.0f);
     }
-    if (tid == kMarkRows - 1) p.counts[blockIdx.x] = before + (live ? 1 : 0);
+    if (tid == static_cast<int>(blockDim.x) - 1) p.counts[blockIdx.x] = before + (live ? 1 : 0);
 }
 
 __device__ __forceinline__ float wave_max(float v) {
@@ -994,7 +999,7 @@ struct RowArgs {
     float* row_losses;
     const int32_t* counts;
     Saved s;
-    int d, row_blocks, biased;
+    int d, row_blocks, mark_rows, biased;
     float inv_t;
 };
 
@@ -1005,7 +1010,7 @@ template <typename E, bool FEW>
 __global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
     constexpr int R = (VMOE_HEAD_MAX_TEACHER + 63) / 64;  // entries a lane
     const int lane = threadIdx.x & 63, wave = wave_id();
-    const int t = blockIdx.x * 4 + wave, mine = blockIdx.x * 4 / kMarkRows;
+    const int t = blockIdx.x * 4 + wave, mine = blockIdx.x * 4 / p.mark_rows;
     const int V = p.told.V, K = p.told.K;
     uint64_t marks = 0;
     if constexpr (FEW) {
@@ -1188,27 +1193,39 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs p) {
 // one CU's share of the bandwidth. Here a block takes all rows against 32 classes: its
 // four waves share k in 128-byte groups, two in flight in registers, which pass through
 // LDS of the wave's own (16-byte chunks XOR-swizzled by row) to be read back as
-// fragments; the waves' sums meet in LDS and are added in wave order.
-constexpr int kFewRows = 64, kFewClasses = 32;
+// fragments; the waves' sums meet in LDS and are added in wave order. z is kept (at
+// most 256 bytes a class, less than the class's weights from d = 128 on in bf16), so the
+// backward reads the weights once: 64 x 1024 against 21841 classes, dz 15 -> 5 us.
 constexpr int kFewLd = kFewClasses + 4;  // floats a row of z in LDS
 
 template <typename E, int RB>
 struct FewLds {
     static constexpr int ROWS = 32 * RB + 32, STAGE = ROWS * 128, PART = RB * 16 * 64 * 4;
-    static constexpr int BYTES = 4 * (STAGE > PART ? STAGE : PART);
+    static constexpr int BYTES = 4 * STAGE;  // the staged groups; then the partial sums, and z
+    static constexpr int Z = 4 * PART;       // behind them
+    static_assert(Z + 32 * RB * kFewLd * 4 <= BYTES, "partial sums and z fit the stages' LDS");
 };
 
-// z of rows [0, rows) and classes [n0, n0 + 32) into zt (bias and all, -infinity past the
-// classes; rows behind the last hold nothing of use).
+// Row r of z in LDS.
+template <typename E, int RB>
+__device__ __forceinline__ float* few_at(char* lds, int r) {
+    return reinterpret_cast<float*>(lds + FewLds<E, RB>::Z) + r * kFewLd;
+}
+
+// z of rows [0, rows) and classes [n0, n0 + 32) into LDS at FewLds::Z (bias and all,
+// -infinity past the classes; rows behind the last hold nothing of use).
 template <typename E, int RB>
 __device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias, int rows, int V,
-                                      int d, int n0, char* lds, float (*zt)[kFewLd]) {
+                                      int d, int n0, char* lds) {
     constexpr int PER = 16 / sizeof(E), GROUP = 8 * PER;  // elements of a chunk, of a group
     constexpr int LA = 4 * RB, LB = 4;
     const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
     const int lr = lane >> 3, lc = PER * (lane & 7);
     const int classes = min(kFewClasses, V - n0);
     const long long row_bytes = static_cast<long long>(d) * sizeof(E);
+    // (wave w's columns of z, see below)
+    const int c = 8 * wave + 4 * h;
+    const float4 bias = *reinterpret_cast<const float4*>(zbias + n0 + c);
     const auto rx = make_rsrc(x, rows * row_bytes);
     const auto rw = make_rsrc(w + static_cast<size_t>(n0) * d, classes * row_bytes);
     const int ng = (d + GROUP - 1) / GROUP, g0 = ng * wave / 4, g1 = ng * (wave + 1) / 4;
@@ -1279,8 +1296,6 @@ __device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias
         for (int q = 0; q < 16; ++q) part[((wave * RB + i) * 16 + q) * 64 + lane] = acc[i][q];
     __syncthreads();
     // wave w: columns 8 w + 4 (lane / 32) + 0..3 of row 32 i + lane % 32
-    const int c = 8 * wave + 4 * h;
-    const float4 bias = *reinterpret_cast<const float4*>(zbias + n0 + c);
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1289,7 +1304,7 @@ __device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 v[q] += part[((w2 * RB + i) * 16 + 4 * wave + q) * 64 + lane];
-        *reinterpret_cast<float4*>(&zt[32 * i + (lane & 31)][c]) =
+        *reinterpret_cast<float4*>(few_at<E, RB>(lds, 32 * i + (lane & 31)) + c) =
             make_float4(v[0] + bias.x, v[1] + bias.y, v[2] + bias.z, v[3] + bias.w);
     }
     __syncthreads();
@@ -1299,27 +1314,31 @@ struct FewStatsArgs {
     Saved s;
     const void* weight;
     float *mx, *sum, *sum_t;  // [strips][N]: a strip is a block's classes
-    int N, V, K, d;
+    int N, V, K, d, vpad;
     float scale, scale_t;
 };
 
 template <typename E, int RB>
-__global__ __launch_bounds__(256) void few_stats_kernel(FewStatsArgs p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3)))
+void few_stats_kernel(FewStatsArgs p) {
     __shared__ __attribute__((aligned(16))) char lds[FewLds<E, RB>::BYTES];
-    __shared__ __attribute__((aligned(16))) float zt[32 * RB][kFewLd];
-    const int tid = threadIdx.x, n0 = blockIdx.x * kFewClasses, live = p.s.head->live;
-    if (live == 0) return;
-    few_z<E, RB>(static_cast<const E*>(p.s.x), static_cast<const E*>(p.weight), p.s.bias, live, p.V,
-                 p.d, n0, lds, zt);
+    const int tid = threadIdx.x, n0 = blockIdx.x * kFewClasses, n = 1 + p.K;
+    // (all N places of rows, so that no load waits for the number of live ones; what is
+    // behind those is left out below. The first targets are requested ahead, too)
+    const int first = tid < p.N * n ? p.s.tidx[tid] : -1;
+    const int live = p.s.head->live;
+    few_z<E, RB>(static_cast<const E*>(p.s.x), static_cast<const E*>(p.weight), p.s.bias, p.N, p.V,
+                 p.d, n0, lds);
     // four threads a row, eight classes each
     const int r = tid >> 2, c0 = 8 * (tid & 3);
     if (r < 32 * RB) {
         float z[8], m = kLowest;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            z[q] = zt[r][c0 + q];
+            z[q] = few_at<E, RB>(lds, r)[c0 + q];
             m = fmaxf(m, z[q]);
         }
+        if (r < live) store8(p.s.z + static_cast<size_t>(r) * p.vpad + n0 + c0, z);
         m = fmaxf(m, __shfl_xor(m, 1, 64));
         m = fmaxf(m, __shfl_xor(m, 2, 64));
         auto total = [&](float scale) {
@@ -1340,48 +1359,41 @@ __global__ __launch_bounds__(256) void few_stats_kernel(FewStatsArgs p) {
         }
     }
     // the logits of the targets among these classes
-    const int n = 1 + p.K;
 #pragma unroll 4
     for (int e = tid; e < live * n; e += 256) {
-        const int c = p.s.tidx[e];
-        if (c >= n0 && c < n0 + kFewClasses) p.s.tz[e] = zt[e / n][c - n0];
+        const int c = e == tid ? first : p.s.tidx[e];
+        if (c >= n0 && c < n0 + kFewClasses) p.s.tz[e] = few_at<E, RB>(lds, e / n)[c - n0];
         else if (c < 0 && blockIdx.x == 0) p.s.tz[e] = 0.0f;
     }
 }
 
 struct FewGradArgs {
     Saved s;
-    const void* weight;  // of the piece
     void* dz;
-    int first, V, K, d, ldz;  // V: classes of the piece
+    int first, cols, K, ldz, vpad;  // the piece's classes
     int mean;
     float w_label, w_teacher, inv_t;
 };
 
-template <typename E, int RB>
+// dz from the z that was kept, eight classes a thread; blockIdx.y: the row.
+template <typename E>
 __global__ __launch_bounds__(256) void few_grad_kernel(FewGradArgs p) {
-    __shared__ __attribute__((aligned(16))) char lds[FewLds<E, RB>::BYTES];
-    __shared__ __attribute__((aligned(16))) float zt[32 * RB][kFewLd];
-    const int tid = threadIdx.x, n0 = blockIdx.x * kFewClasses;
+    const int r = blockIdx.y, c = 8 * (blockIdx.x * 256 + threadIdx.x);
     const Header h = *p.s.head;
-    if (h.live == 0) return;
-    few_z<E, RB>(static_cast<const E*>(p.s.x), static_cast<const E*>(p.weight),
-                 p.s.bias + p.first, h.live, p.V, p.d, n0, lds, zt);
-    const int r = tid >> 2, c0 = 8 * (tid & 3);
-    if (r >= h.live) return;
+    if (r >= h.live || c >= p.cols) return;
+    float v[8];
+    load8(p.s.z + static_cast<size_t>(r) * p.vpad + p.first + c, v);
     const float4 rec = p.s.rec[r];
     const float2 g = Rates(h, p.w_label, p.w_teacher, p.mean).of(p.s.weight[r]);
     const Softmax soft(h, p.K > 0, p.inv_t);
     // (with a teacher, subtract_kernel sees to the targets)
-    const int label = p.K == 0 ? p.s.tidx[r] - p.first - n0 - c0 : -1;
-    float v[8];
+    const int label = p.K == 0 ? p.s.tidx[r] - p.first - c : -1;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-        const float z = zt[r][c0 + q];
-        v[q] = soft.two ? soft.at<true>(z, rec, g) : soft.at<false>(z, rec, g);
+        v[q] = soft.two ? soft.at<true>(v[q], rec, g) : soft.at<false>(v[q], rec, g);
         if (q == label) v[q] -= g.x;
     }
-    store8(static_cast<E*>(p.dz) + static_cast<size_t>(r) * p.ldz + n0 + c0, v);
+    store8(static_cast<E*>(p.dz) + static_cast<size_t>(r) * p.ldz + c, v);
 }
 
 // ------------------------------------------------------------------ losses
@@ -1758,8 +1770,8 @@ Cut choose_cut(const vmoe_head_shape& s, long long cols) {
             for (const int w : ranges) {
                 if (w > 1 && (w > sw || w > 16 || tw * w > 4 * cus)) break;
                 const double time_w = stage * ((sw + w - 1) / w + extra);
-                const double c = ends_at(cus, tx * x, time_x, tw * w, time_w) +
-                                 part * (tx * x + (w > 1 ? tw * w : 0.0));
+                double c = ends_at(cus, tx * x, time_x, tw * w, time_w) + part * tx * x;
+                if (w > 1) c += part * tw * w + 3.0;  // and a launch
                 if (c < least) {
                     least = c;
                     best = Cut{narrow, x, w};
@@ -1807,7 +1819,7 @@ static_assert(TileBig::BN == 256 && TileBig::WGN == 2 && F32Tile::BN == 128 && F
               "two strips a tile of z");
 
 struct FwdPlan {
-    int few, row_blocks, strips, finish_rows, finish_blocks, two;
+    int few, mark_rows, row_blocks, strips, finish_rows, finish_blocks, two;
     int tile_rows, tile_shift, tiles_n;  // of z
     size_t counts_off, ticket_off, sums_off, mx_off, sum_off, sumt_off, list_off, ends_off, bytes;
 };
@@ -1815,14 +1827,16 @@ struct FwdPlan {
 FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     FwdPlan p;
     const size_t N = s.n_rows;
-    p.row_blocks = static_cast<int>(cdiv(s.n_rows, kMarkRows));
+    // (a block of rows_kernel adds up the counts of the blocks before it)
+    p.mark_rows = s.n_rows <= 65536 ? 256 : 1024;
+    p.row_blocks = static_cast<int>(cdiv(s.n_rows, p.mark_rows));
     p.tile_rows = s.dtype == VMOE_BF16 ? TileBig::BM : F32Tile::BM;
     p.tile_shift = s.dtype == VMOE_BF16 ? 8 : 7;
     p.tiles_n = static_cast<int>(cdiv(s.n_classes, 1 << p.tile_shift));
     p.few = s.n_rows <= kFewRows;
     p.strips = p.few ? static_cast<int>(cdiv(s.n_classes, kFewClasses)) : 2 * p.tiles_n;
     // few rows: four lanes a row, since many strips stand before each
-    p.finish_rows = s.n_rows <= 1024 ? 16 : 64;
+    p.finish_rows = s.n_rows <= 2048 ? 16 : 64;
     p.finish_blocks = s.n_rows > 0 ? static_cast<int>(cdiv(s.n_rows, p.finish_rows)) : 1;
     p.two = labels && s.n_teacher > 0 && s.temperature != 1.0f;
     Carver c{nullptr};
@@ -1901,8 +1915,8 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
                      reinterpret_cast<int32_t*>(base + p.counts_off), p.row_blocks};
     const bool bf16 = s.dtype == VMOE_BF16;
     const float inv_t = 1.0f / s.temperature;
-    const RowArgs t{x, told, zb, row_losses, m.counts, v, s.d_model, p.row_blocks, bias != nullptr,
-                    inv_t};
+    const RowArgs t{x, told, zb, row_losses, m.counts, v, s.d_model, p.row_blocks, p.mark_rows,
+                    bias != nullptr, inv_t};
     const unsigned row_grid = N > 0 ? cdiv(N, 4) : 1;
     float* const mx = reinterpret_cast<float*>(base + p.mx_off);
     float* const sum = reinterpret_cast<float*>(base + p.sum_off);
@@ -1912,17 +1926,17 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
         const unsigned grid = row_grid + cdiv(zb.vpad, 256);
         if (bf16) rows_kernel<uint16_t, true><<<grid, 256, 0, st>>>(t);
         else rows_kernel<float, true><<<grid, 256, 0, st>>>(t);
-        const FewStatsArgs a{v, weight, mx, sum, sum_t, N, V, K, s.d_model, kLog2e * inv,
-                             kLog2e * inv_t};
+        const FewStatsArgs a{v, weight, mx, sum, sum_t, N, V, K, s.d_model, zb.vpad,
+                             kLog2e * inv, kLog2e * inv_t};
         auto go = [&](auto blocks) {
             constexpr int RB = decltype(blocks)::value;
             if (bf16) few_stats_kernel<uint16_t, RB><<<p.strips, 256, 0, st>>>(a);
             else few_stats_kernel<float, RB><<<p.strips, 256, 0, st>>>(a);
         };
-        if (N <= 32) go(std::integral_constant<int, 1>{});
-        else go(std::integral_constant<int, 2>{});
+        if (N > 32) go(std::integral_constant<int, 2>{});
+        else if (N > 0) go(std::integral_constant<int, 1>{});
     } else {
-        mark_kernel<<<p.row_blocks + cdiv(zb.vpad, kMarkRows), kMarkRows, 0, st>>>(m);
+        mark_kernel<<<p.row_blocks + cdiv(zb.vpad, p.mark_rows), p.mark_rows, 0, st>>>(m);
         if (bf16) rows_kernel<uint16_t, false><<<row_grid, 256, 0, st>>>(t);
         else rows_kernel<float, false><<<row_grid, 256, 0, st>>>(t);
         const SortArgs g{v, reinterpret_cast<uint32_t*>(base + p.list_off),
@@ -1999,16 +2013,13 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
         z.label = z.teacher ? nullptr : v.tidx;
         z.first = first;
         if (N <= kFewRows) {
-            const FewGradArgs u{v, w, z.dz, first, count, s.n_teacher, d, z.ldz, z.mean,
-                                z.w_label, z.w_teacher, z.inv_t};
-            const unsigned grid = cdiv(count, kFewClasses);
-            auto go = [&](auto blocks) {
-                constexpr int RB = decltype(blocks)::value;
-                if (bf16) few_grad_kernel<uint16_t, RB><<<grid, 256, 0, st>>>(u);
-                else few_grad_kernel<float, RB><<<grid, 256, 0, st>>>(u);
-            };
-            if (N <= 32) go(std::integral_constant<int, 1>{});
-            else go(std::integral_constant<int, 2>{});
+            // (the forward wrote z of whole blocks of classes)
+            const int cols = static_cast<int>(cdiv(count, kFewClasses)) * kFewClasses;
+            const FewGradArgs u{v, z.dz, first, cols, s.n_teacher, z.ldz, padded_classes(s),
+                                z.mean, z.w_label, z.w_teacher, z.inv_t};
+            const dim3 grid(cdiv(cols, 2048), N);
+            if (N > 0 && bf16) few_grad_kernel<uint16_t><<<grid, 256, 0, st>>>(u);
+            else if (N > 0) few_grad_kernel<float><<<grid, 256, 0, st>>>(u);
         } else {
             launch_logits(s, z, st);
         }
