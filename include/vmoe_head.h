@@ -25,7 +25,7 @@ typedef enum { VMOE_REDUCE_MEAN = 0, VMOE_REDUCE_SUM = 1 } vmoe_reduction;
 #define VMOE_HEAD_MAX_TEACHER 256
 
 typedef struct vmoe_head_shape {
-    int32_t n_rows;      /* N >= 0, at most 2^21 (else UNSUPPORTED)                   */
+    int32_t n_rows;      /* N >= 0, at most 2^21 in bf16, 2^20 in f32 (else UNSUPPORTED) */
     int32_t d_model;     /* d, multiple of 8, at most 65536; x below 2 GiB (else
                             UNSUPPORTED)                                              */
     int32_t n_classes;   /* V >= 1, at most 2^21; N V < 2^36 (else UNSUPPORTED)       */
@@ -83,6 +83,7 @@ vmoe_status vmoe_head_loss_fwd(const vmoe_head_shape* shape, const void* x, cons
  *   dx = dz weight [N, d] (0 for rows that were left out),
  *   dweight = dz^T x [V, d], dbias = sum_t dz [V]               dtype, overwritten
  * Each of them may be NULL and is not formed then (a frozen head, or a head alone).
+ * VMOE_ERR_INVALID_ARG for weights that are not finite, w_teacher T included.
  * The logits of more than 64 rows are formed again. bf16: dz is rounded to bf16 for the
  * products, as every operand of theirs is; they and the sums accumulate in f32 and are
  * rounded once.

@@ -20,7 +20,8 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
 
 namespace {
 
-constexpr int kMaxRows = 1 << 21, kMaxClasses = 1 << 21, kMaxWidth = 1 << 16;
+constexpr int kMaxRowBytes = 1 << 22;  // N times an element's: a piece of 256 classes within 1 GiB
+constexpr int kMaxClasses = 1 << 21, kMaxWidth = 1 << 16;
 constexpr long long kMaxTokenBytes = 1LL << 31;  // N d: 32-bit offsets
 constexpr long long kMaxLogits = 1LL << 36;   // N V: threads of one launch
 constexpr float kMaxTemperature = 1024.0f;
@@ -35,9 +36,9 @@ vmoe_status check_shape(const vmoe_head_shape* s) {
         return VMOE_ERR_INVALID_ARG;
     if (!(s->temperature >= 1.0f / kMaxTemperature && s->temperature <= kMaxTemperature))
         return VMOE_ERR_INVALID_ARG;
-    const long long n = s->n_rows;
-    if (s->n_rows > kMaxRows || s->n_classes > kMaxClasses || s->d_model > kMaxWidth ||
-        n * s->d_model * (s->dtype == VMOE_BF16 ? 2 : 4) >= kMaxTokenBytes || n * s->n_classes >= kMaxLogits)
+    const long long n = s->n_rows, size = s->dtype == VMOE_BF16 ? 2 : 4;
+    if (n * size > kMaxRowBytes || s->n_classes > kMaxClasses || s->d_model > kMaxWidth ||
+        n * s->d_model * size >= kMaxTokenBytes || n * s->n_classes >= kMaxLogits)
         return VMOE_ERR_UNSUPPORTED;
     return VMOE_OK;
 }
@@ -95,7 +96,7 @@ vmoe_status vmoe_head_loss_bwd(const vmoe_head_shape* shape, const void* weight,
                                size_t workspace_bytes, void* stream) {
     VMOE_TRY(check_shape(shape));
     VMOE_TRY(need(dev(weight) && dev(saved) && opt(dx) && opt(dweight) && opt(dbias)));
-    VMOE_TRY(need(isfinite(w_label) && isfinite(w_teacher)));
+    VMOE_TRY(need(isfinite(w_label) && isfinite(w_teacher * shape->temperature)));
     VMOE_TRY(need(dx || dweight || dbias));
     if (workspace_bytes < head_bwd_workspace_bytes(*shape) || !dev(workspace))
         return VMOE_ERR_WORKSPACE;

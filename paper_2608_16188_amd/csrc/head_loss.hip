@@ -37,8 +37,9 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kCus = 256;
 constexpr size_t kPieceBytes = size_t(1) << 30;  // dz of one piece of the classes
 // Stands for the maximum of a strip without a class: its -infinities give sums of 0
-// (with -infinity itself, differences would be NaN).
-constexpr float kLowest = -1e30f;
+// (with -infinity itself, differences would be NaN). A power of two, whose products with
+// a scale are exact: RowSums::join takes their rounding for an exponent.
+constexpr float kLowest = -0x1p100f;
 
 size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
@@ -204,6 +205,7 @@ struct Rates {
             label = h.sum[0] != 0.0f ? label / h.sum[0] : 0.0f;
             teacher = h.sum[1] != 0.0f ? teacher / h.sum[1] : 0.0f;
         }
+        if (!h.labelled) label = 0.0f;  // (the weight of a teacher that is not there is 0)
         all = fmaxf(fabsf(label), fabsf(teacher));
         if (all > 0.0f) {
             label /= all;
@@ -1984,7 +1986,7 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
     const int N = s.n_rows, V = s.n_classes, d = s.d_model;
     const size_t size = elem_bytes(s);
     const bool bf16 = s.dtype == VMOE_BF16;
-    const Factor factor{v.head, w_label, w_teacher * s.temperature,
+    const Factor factor{v.head, w_label, s.n_teacher > 0 ? w_teacher * s.temperature : 0.0f,
                         s.reduction == VMOE_REDUCE_MEAN};
     for (int i = 0; i < p.pieces; ++i) {
         const int first = i * p.cols, count = min(p.cols, V - first);

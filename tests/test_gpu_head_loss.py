@@ -29,6 +29,11 @@ CASES = {
     "one_class": Case(5, 8, 1, k=1, t=2.0),
     "two_classes_f32": Case(9, 16, 2, k=2, t=0.5, dtype="f32"),
     "narrow": Case(33, 8, 100, k=3),
+    # waves whose strips hold no class, at scales that are no powers of two
+    **{f"few_classes_t{t}": Case(n, 16, 10, k=2, t=t, dtype=dt, labels=lab)
+       for t, n, dt, lab in ((3.0, 5, "bf16", True), (0.7, 70, "bf16", True),
+                             (1.5, 70, "f32", False), (5.3, 300, "f32", True),
+                             (0.11, 9, "f32", False), (11.0, 90, "bf16", False))},
     "tile_edge_below": Case(255, 72, 255, ignored=0.2),
     "tile_edge": Case(256, 64, 256, weighted=True),
     "tile_edge_above": Case(257, 192, 257, k=5, t=2.0),
@@ -145,6 +150,47 @@ def test_weights_of_the_losses(dtype):
         ref, bound = d.reference(w1=w1, w2=w2)
         for k in got:
             close(k, got[k], ref[k], bound[k])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n, reduction", [(40, 0), (300, 0), (300, 1)])
+def test_rows_of_negative_weight(dtype, n, reduction):
+    c = Case(n, 64, 200, k=3, t=2.0, dtype=dtype, reduction=reduction)
+    d = Data(c)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    d.row_weight = torch.randn(n, device="cuda", generator=g) + 0.5
+    check(c, d)
+    label = Data(Case(n, 64, 200, dtype=dtype, reduction=reduction))
+    label.row_weight = d.row_weight
+    check(label.case, label)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_weight_of_a_loss_that_is_not_there(dtype):
+    """However large it is, it moves nothing."""
+    for kw in (dict(), dict(k=3, labels=False)):
+        d = Data(Case(100, 64, 300, dtype=dtype, reduction=H.VMOE_REDUCE_SUM, **kw))
+        big = dict(w1=1.0, w2=1e30) if d.case.labels else dict(w1=1e30, w2=1.0)
+        a, b = d.run(w1=1.0, w2=1.0), d.run(**big)
+        for k in a:
+            assert same_bits(a[k], b[k]), k
+
+
+def test_weights_beyond_2_gib():
+    """Offsets past 32 bits in the head's weight and its gradient, and several pieces."""
+    n, d, v = 70, 1024, 1100003
+    assert v * d * 2 > 2 ** 31
+    c = Case(n, d, v, k=2, t=2.0, bias=False)
+    data = Data(c)
+    data.labels[:4] = torch.tensor([v - 1, v - 2, 0, v - 300], dtype=torch.int32)
+    say("head loss beyond 2 GiB", c)
+    got = data.run(want=("dx", "dweight"))
+    ref, bound = data.reference()
+    for k in ("losses", "row_losses", "dx"):
+        close(k, got[k], ref[k], bound[k])
+    for rows in (slice(0, 300), slice(v // 2, v // 2 + 300), slice(v - 300, v)):
+        close("dweight", got["dweight"][rows], ref["dweight"][rows], bound["dweight"][rows])
+    torch.cuda.empty_cache()
 
 
 def test_several_backwards_of_one_forward():

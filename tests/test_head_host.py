@@ -56,6 +56,7 @@ REFUSED = [
     (dict(temperature=math.nan), BAD), (dict(temperature=math.inf), BAD),
     (dict(temperature=2.0 ** -11), BAD), (dict(temperature=1025.0), BAD),
     (dict(n_rows=2 ** 21 + 1, d_model=8, n_classes=1), UNS),
+    (dict(n_rows=2 ** 20 + 1, d_model=8, n_classes=1, dtype=V.VMOE_F32), UNS),
     (dict(n_classes=2 ** 21 + 1, n_rows=1), UNS), (dict(d_model=65544, n_rows=1), UNS),
     (dict(n_rows=2 ** 20, d_model=1024), UNS),
     (dict(n_rows=2 ** 19, d_model=1024, dtype=V.VMOE_F32), UNS),
@@ -127,6 +128,12 @@ def test_arguments_of_the_backward_refused(kw, status):
     assert call("vmoe_head_loss_bwd", ctypes.addressof(_shape()), *a.values(), None) == status
 
 
+def test_a_teachers_weight_that_overflows_refused():
+    s = _shape(n_teacher=2, temperature=1024.0)
+    assert call("vmoe_head_loss_bwd", ctypes.addressof(s), FAKE, FAKE, 1.0, 1e36, FAKE, FAKE, FAKE,
+                FAKE, H.vmoe_head_loss_bwd_workspace_bytes(s), None) == BAD
+
+
 @pytest.mark.parametrize("n, d, v, k", [
     (0, 8, 1, 0), (1, 8, 1, 256), (64, 768, 1000, 10), (65, 768, 1000, 10), (6304, 768, 50000, 0),
     (36928, 1024, 32000, 64), (2 ** 21, 8, 2 ** 14, 0), (1, 65536, 2 ** 21, 0),
@@ -139,7 +146,7 @@ def test_buffers_do_not_grow_with_the_logits(n, d, v, k, dtype):
     ranges and of a piece's dweight in up to 16 (only where either has few tiles)."""
     s = _shape(n_rows=n, d_model=d, n_classes=v, n_teacher=k, dtype=dtype)
     size = 2 if dtype == V.VMOE_BF16 else 4
-    if n * d * size >= 2 ** 31:
+    if n * d * size >= 2 ** 31 or n * size > 2 ** 22:
         assert SIZES[0](s) == 0
         return
     saved, fwd, bwd = (f(s) for f in SIZES)
