@@ -271,6 +271,8 @@ def main():
                     help="classes of a teacher's list for each token (with --classes)")
     ap.add_argument("--temperature", type=float, default=2.0, help="of the distillation")
     a = ap.parse_args()
+    if a.classes < 0 or not 0 <= a.teacher_top <= min(a.classes, H.MAX_TEACHER):
+        ap.error(f"--teacher-top: at most --classes and {H.MAX_TEACHER}")
     cfg = W.CONFIGS[a.workload]
     inputs = W.make_inputs(cfg)
     options = dict(state_bits=a.state_bits, row_scale=False)

@@ -427,8 +427,8 @@ PyMethodDef methods[] = {method<block_norm_fwd>("block_norm_fwd"),
                          method<adamw_state_values>("adamw_state_values"),
                          {nullptr, nullptr, 0, nullptr}};
 
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train", "Calls of vmoe_train.h and vmoe_head.h", -1, methods,
-                      nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train", "Calls of vmoe_train.h and vmoe_head.h", -1,
+                      methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

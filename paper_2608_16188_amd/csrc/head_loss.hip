@@ -578,8 +578,9 @@ __device__ __forceinline__ void put_block(const f32x16& v, lds_u16* s) {
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<lds_v4*>(s + r * 64 + (((2 * q + h) ^ (r & 7)) << 3)) = __builtin_bit_cast(
-            v4i32, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
+        *reinterpret_cast<lds_v4*>(s + r * 64 + (((2 * q + h) ^ (r & 7)) << 3)) =
+            __builtin_bit_cast(v4i32,
+                               make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
 }
 
 // LDS of a wave's own, 4 KB.
@@ -1491,8 +1492,11 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
             if (k >= live) break;
             const size_t entry = static_cast<size_t>(k) * (1 + p.K) + 1;
             float v = 0.0f;
-            for (int j = lane; j < p.K; j += 64)
-                v = __builtin_fmaf(p.s.tq[entry + j], p.s.tz[entry + j] * p.inv_t, v);
+            for (int j = lane; j < p.K; j += 64) {
+                const float q = p.s.tq[entry + j], zt = p.s.tz[entry + j] * p.inv_t;
+                // (an entry without a share adds nothing, of a class masked out neither)
+                v = __builtin_fmaf(q, q == 0.0f ? 0.0f : zt, v);
+            }
             v = wave_total(v);
             if (lane == 0) cross_s[u] = v;
         }
@@ -2103,11 +2107,11 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             constexpr int G = decltype(groups)::value;
             const unsigned grid = cdiv(static_cast<long long>(N) * (d / 8), 256 / G);
             if (bf16)
-                dx_kernel<uint16_t, G><<<grid, 256, 0, st>>>(part, stride, p.cut.dx, v.place,
-                                                             static_cast<uint16_t*>(dx), N, d, factor);
+                dx_kernel<uint16_t, G><<<grid, 256, 0, st>>>(
+                    part, stride, p.cut.dx, v.place, static_cast<uint16_t*>(dx), N, d, factor);
             else
-                dx_kernel<float, G><<<grid, 256, 0, st>>>(part, stride, p.cut.dx, v.place,
-                                                          static_cast<float*>(dx), N, d, factor);
+                dx_kernel<float, G><<<grid, 256, 0, st>>>(
+                    part, stride, p.cut.dx, v.place, static_cast<float*>(dx), N, d, factor);
         };
         if (p.cut.dx >= 16) go(std::integral_constant<int, 8>{});
         else go(std::integral_constant<int, 1>{});

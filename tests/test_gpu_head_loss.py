@@ -58,6 +58,12 @@ CASES = {
     "empty": Case(0, 64, 700, k=4),
     "summed": Case(200, 64, 300, k=4, t=2.0, reduction=H.VMOE_REDUCE_SUM, weighted=True,
                    ignored=0.1),
+    "few_rows_at_most": Case(64, 72, 1001, k=5, t=2.0, weighted=True, missing=0.2),
+    "few_rows_at_most_f32": Case(64, 72, 1001, k=5, t=2.0, dtype="f32", ignored=0.3),
+    "few_rows_passed": Case(65, 72, 1001, k=5, t=2.0, weighted=True, missing=0.2),
+    "few_rows_passed_f32": Case(65, 72, 1001, k=5, t=2.0, dtype="f32", ignored=0.3),
+    "row_blocks_of_1024": Case(70001, 16, 33, k=2, t=2.0, ignored=0.4, weighted=True),
+    "row_blocks_of_1024_f32": Case(66000, 8, 17, dtype="f32", ignored=0.7),
     "mark_blocks": Case(2100, 64, 90, k=2, ignored=0.5, weighted=True),
     "wide": Case(20, 4096, 500),
     "wide_f32": Case(20, 2056, 500, dtype="f32", k=3, t=2.0),
@@ -258,6 +264,44 @@ def test_weights_that_cancel(dtype):
     for k in ("dx", "dweight", "dbias"):
         assert (got[k] == 0).all(), k
     assert (got["row_losses"][:, 0] > 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [40, 200])
+@pytest.mark.parametrize("t", [1.0, 1.7])
+@pytest.mark.parametrize("lowest", [False, True])
+def test_classes_masked_by_the_bias(dtype, n, t, lowest):
+    """-infinity, or the type's lowest value, at classes that are not to be there, whole
+    strips of them too: as a head over the others. An entry of such a class that has
+    no share of its list (exp(-200) is 0 in f32) takes no part."""
+    v = 700
+    c = Case(n, 64, v, k=4, t=t, dtype=dtype)
+    d = Data(c)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    keep = torch.rand(v, device="cuda", generator=g) < 0.6
+    keep[256:520] = False
+    kept = torch.nonzero(keep)[:, 0]
+    pick = lambda *s: kept[torch.randint(0, len(kept), s, device="cuda",  # noqa: E731
+                                         generator=g)].to(torch.int32)
+    d.labels, d.idx = pick(n), pick(n, 4)
+    d.idx[::2, 3] = 300
+    d.logits[::2, 3] = -200.0 * t
+    mask = torch.finfo(d.bias.dtype).min if lowest else -math.inf
+    d.bias = torch.where(keep, d.bias, mask)
+    got = d.run()
+    to = torch.full((v,), -1, dtype=torch.int32, device="cuda")
+    to[kept] = torch.arange(len(kept), dtype=torch.int32, device="cuda")
+    few = Data(Case(n, 64, len(kept), k=4, t=t, dtype=dtype))
+    few.x, few.weight, few.bias = d.x, d.weight[kept], d.bias[kept]
+    few.labels, few.idx, few.logits = to[d.labels.long()], to[d.idx.long()], d.logits
+    ref, bound = few.reference()
+    # (the bounds' counts of strips and of sums over classes are of 700 here)
+    more = 1.0 + (v + 80) / (len(kept) + 80)
+    for k in ("losses", "row_losses", "dx"):
+        close(k, got[k], ref[k], more * bound[k])
+    for k in ("dweight", "dbias"):
+        close(k, got[k][kept], ref[k], more * bound[k])
+        assert (got[k][~keep] == 0).all(), k
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
