@@ -36,10 +36,11 @@ typedef struct vmoe_head_shape {
     int32_t reserved;    /* must be 0                                                 */
 } vmoe_head_shape;
 
-/* Bytes of `saved` and of the calls' scratch (0 on an invalid shape). Neither
- * grows with N V, but for at most 64 rows, whose logits `saved` holds: those of more
- * rows are formed a tile at a time and never stored, and their gradient a piece of the
- * classes at a time, within 1 GiB of the workspace. */
+/* Bytes of `saved` and of the calls' scratch (0 on an invalid shape). `saved` holds the
+ * logits (4 N V bytes, V up to a multiple of 32) of at most 64 rows, of at most some
+ * 4 million logits, or, in f32, of at most 64 million; others are formed a tile at a
+ * time, never stored, and formed again by the backward, so that nothing grows with N V.
+ * dz is formed a piece of the classes at a time, within 1 GiB of the workspace. */
 size_t vmoe_head_loss_saved_bytes(const vmoe_head_shape* shape);
 size_t vmoe_head_loss_fwd_workspace_bytes(const vmoe_head_shape* shape);
 size_t vmoe_head_loss_bwd_workspace_bytes(const vmoe_head_shape* shape);
@@ -84,9 +85,8 @@ vmoe_status vmoe_head_loss_fwd(const vmoe_head_shape* shape, const void* x, cons
  *   dweight = dz^T x [V, d], dbias = sum_t dz [V]               dtype, overwritten
  * Each of them may be NULL and is not formed then (a frozen head, or a head alone).
  * VMOE_ERR_INVALID_ARG for weights that are not finite, w_teacher T included.
- * The logits of more than 64 rows are formed again. bf16: dz is rounded to bf16 for the
- * products, as every operand of theirs is; they and the sums accumulate in f32 and are
- * rounded once.
+ * bf16: dz is rounded to bf16 for the products, as every operand of theirs is; they and
+ * the sums accumulate in f32 and are rounded once.
  * `saved` is read only: several backwards may follow one forward. */
 vmoe_status vmoe_head_loss_bwd(const vmoe_head_shape* shape, const void* weight,
                                const void* saved, float w_label, float w_teacher, void* dx,

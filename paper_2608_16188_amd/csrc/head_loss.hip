@@ -1,20 +1,19 @@
 // A head over many classes with its losses (vmoe_head.h) on gfx950.
 //
-// z = x W^T + b of more than 64 rows is never stored. The forward forms it a tile at a
-// time and keeps of each row and strip of columns the largest value and the sum of
+// z = x W^T + b is not stored, but for few logits. The forward forms it a tile at a time
+// and keeps of each row and strip of columns the largest value and the sum of
 // exponentials; the backward forms it again, turns it into dz a piece of the classes at
-// a time and multiplies that piece by W and by x (the kernels of at most 64 rows keep z,
-// V times 256 bytes at most, and read it back):
+// a time and multiplies that piece by W and by x (few logits are kept and read back):
 //   mark      which rows have a label or a teacher, their places among those
 //             (256 or 1024 rows a block); the bias in f32, -infinity past the classes
 //   rows      a wave a row: the row's x to its place, its label and its teacher's
 //             entries with their q
 //   sort      with a teacher, the entries by the tile of z that they lie in
 //   stats     z by tiles -> (max, sum of exponentials) of each row and strip, and the
-//             logits of labels and entries
+//             logits of labels and entries; or z itself (then without sort)
 //   finish    lse of each row, its losses, their sums (last block, double)
 // and for each piece of the classes
-//   grad_z    z by tiles -> dz, in the operands' type
+//   grad_z    z by tiles, or as it was kept -> dz, in the operands' type
 //   subtract  with a teacher, dz at the targets, in f32 from their logits, rounded once
 //   products  dx += dz W (f32 partial sums in slots), dW = dz^T x, db = sums of dz
 // and in the end dx from the slots, rounded once, rows back to their places.
@@ -23,7 +22,9 @@
 //
 // z twice costs 2 N V d products more than the 6 N V d of keeping it; kept in f32 it
 // would be written, read and written again as dz, 10 bytes a logit: at 5 TB/s and
-// 1 PFLOP/s as long as the products at d = 1024, and memory that grows with N V.
+// 1 PFLOP/s as long as the products at d = 1024, and memory that grows with N V. So it is
+// kept where the products do not fill the GPU anyway, and in f32, whose products are
+// eight times as long, up to 256 MiB.
 #include <math.h>
 
 #include "../../include/vmoe_head.h"
@@ -67,12 +68,35 @@ struct Saved {
     float* tz;       // [N, 1 + K] their logits
     float* tq;       // [N, 1 + K] 1 and q
     void* x;         // [N, d]
-    float* z;        // [N, V up to 256] of few rows
+    float* z;        // [N, V up to 32] where it is kept
     size_t bytes;
 };
 
-// At most so many rows take the kernels of few rows.
+// Few logits, which have a kernel of their own: at most kFewRows rows, or a number of
+// blocks of kFewRows rows and kFewClasses classes. Tiles win from some 2048 blocks on in
+// bf16 (4096 x 1024 rows against 1000 classes 120 us with tiles, 99 with blocks;
+// 6304 x 768, 3168 blocks: 112, 118), from some 768 in f32, whose tiles are smaller
+// (1024 x 1024 against 1000, 512 blocks: 110, 97; 2048 x 1024, 1024 blocks: 150, 156).
 constexpr int kFewRows = 64, kFewClasses = 32;
+bool few_logits(const vmoe_head_shape& s) {
+    const long long rows = (s.n_rows + kFewRows - 1LL) / kFewRows;
+    return s.n_rows <= kFewRows ||
+           rows * ((s.n_classes + kFewClasses - 1) / kFewClasses) <=
+               (s.dtype == VMOE_BF16 ? 2048 : 768);
+}
+int kept_classes(const vmoe_head_shape& s) {
+    return (s.n_classes + kFewClasses - 1) / kFewClasses * kFewClasses;
+}
+
+// Whether the forward leaves z for the backward: written once and read once, 8 bytes
+// against 2 d operations a logit. In f32 that pays from d = 192 on (512 x 768 against
+// 32000 classes 900 -> 722 us, 552 x 192 against 100000 980 -> 855).
+constexpr long long kMostKept = 1 << 26;
+bool keeps_logits(const vmoe_head_shape& s) {
+    return few_logits(s) ||
+           (s.dtype != VMOE_BF16 && s.d_model >= 192 &&
+            static_cast<long long>(s.n_rows) * kept_classes(s) <= kMostKept);
+}
 
 int padded_classes(const vmoe_head_shape& s) { return static_cast<int>(up256(s.n_classes)); }
 size_t elem_bytes(const vmoe_head_shape& s) { return s.dtype == VMOE_BF16 ? 2 : 4; }
@@ -102,7 +126,7 @@ Saved saved_layout(const vmoe_head_shape& s, void* base) {
     v.tz = c.take<float>(E);
     v.tq = c.take<float>(E);
     v.x = c.take<char>(N * s.d_model * elem_bytes(s));
-    v.z = c.take<float>(N <= kFewRows ? N * padded_classes(s) : 0);
+    v.z = c.take<float>(keeps_logits(s) ? N * kept_classes(s) : 0);
     v.bytes = c.off;
     return v;
 }
@@ -148,7 +172,8 @@ struct StatsArgs : Product {
     float* tz;                // and where their logits go, and the entries'
     const uint32_t* list;     // entries by tile (sort_kernel), or null
     const int32_t* ends;
-    int n_rows, per_row, has_bias;
+    float* z;                 // f32: [N, ldk], where z is kept (then without tz and list)
+    int n_rows, per_row, has_bias, ldk;
     float scale, scale_t;     // log2 e / temperature of `sum` and of `sum_t`
     static constexpr int OUT = EPI_STORE;
     static constexpr bool A_KMAJOR = true, B_KMAJOR = true;
@@ -637,10 +662,22 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, Sta
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int wm = wave / T::WGN, wn = wave % T::WGN;
     if (p.has_bias || N < T::BN) add_bias<T>(acc, p.zbias, p.t_n0);
+    const bool keep = is_f32<T>() && p.z != nullptr;
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         if (i >= fm_live) break;
         const int r0 = T::WM * wm + 32 * i;
+        if constexpr (is_f32<T>()) {
+            if (keep) {
+#pragma unroll
+                for (int b = 0; b < T::PB; ++b) {
+                    const int n = p.t_n0 + 64 * b + 32 * wn;
+                    store_block(acc[i][b], wave_lds(arrays),
+                                p.z + static_cast<size_t>(p.t_m0 + r0) * p.ldk + n, p.ldk, M - r0,
+                                p.ldk - n);
+                }
+            }
+        }
         const size_t row = p.t_m0 + min(r0 + (lane & 31), M - 1);
         const int spot = class_spot<T>(p.ahead.label[i], p.t_n0);
         float m = kLowest;
@@ -671,7 +708,7 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, Sta
             const float st = total(p.scale_t);
             if (store) p.sum_t[at] = st;
         }
-        if (__any(spot >= 0)) {  // (few strips hold a label)
+        if (!keep && __any(spot >= 0)) {  // (few strips hold a label)
             float z = 0.0f;
 #pragma unroll
             for (int b = 0; b < T::PB; ++b)
@@ -1189,16 +1226,16 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs p) {
     });
 }
 
-// ------------------------------------------------------------------ few rows
+// ------------------------------------------------------------------ few logits
 
-// At most 64 rows: a block of 256 x 256 tiles would leave most of its waves without a
-// row and most CUs without a tile, each streaming half a megabyte of weights through
-// one CU's share of the bandwidth. Here a block takes all rows against 32 classes: its
-// four waves share k in 128-byte groups, two in flight in registers, which pass through
-// LDS of the wave's own (16-byte chunks XOR-swizzled by row) to be read back as
-// fragments; the waves' sums meet in LDS and are added in wave order. z is kept (at
-// most 256 bytes a class, less than the class's weights from d = 128 on in bf16), so the
-// backward reads the weights once: 64 x 1024 against 21841 classes, dz 15 -> 5 us.
+// Few rows or few logits: a block of 256 x 256 tiles would leave most of its waves
+// without a row or most CUs without a tile, each streaming half a megabyte of weights
+// through one CU's share of the bandwidth. Here a block takes 64 rows against 32
+// classes: its four waves share k in 128-byte groups, two in flight in registers, which
+// pass through LDS of the wave's own (16-byte chunks XOR-swizzled by row) to be read back
+// as fragments; the waves' sums meet in LDS and are added in wave order. z is kept, so the
+// backward reads the weights once. 64 x 1024 against 21841 classes: 15.6 us here, 45 MB
+// of weights at 2.9 TB/s; 1024 x 1024 against 1000 forward and backward 100 -> 61 us.
 constexpr int kFewLd = kFewClasses + 4;  // floats a row of z in LDS
 
 template <typename E, int RB>
@@ -1218,8 +1255,8 @@ __device__ __forceinline__ float* few_at(char* lds, int r) {
 // z of rows [0, rows) and classes [n0, n0 + 32) into LDS at FewLds::Z (bias and all,
 // -infinity past the classes; rows behind the last hold nothing of use).
 template <typename E, int RB>
-__device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias, int rows, int V,
-                                      int d, int n0, char* lds) {
+__device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias, int rows,
+                                      int live, int V, int d, int n0, char* lds) {
     constexpr int PER = 16 / sizeof(E), GROUP = 8 * PER;  // elements of a chunk, of a group
     constexpr int LA = 4 * RB, LB = 4;
     const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
@@ -1229,6 +1266,7 @@ __device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias
     // (wave w's columns of z, see below)
     const int c = 8 * wave + 4 * h;
     const float4 bias = *reinterpret_cast<const float4*>(zbias + n0 + c);
+    const bool half = RB > 1 && live <= 32;  // no row behind the first 32
     const auto rx = make_rsrc(x, rows * row_bytes);
     const auto rw = make_rsrc(w + static_cast<size_t>(n0) * d, classes * row_bytes);
     const int ng = (d + GROUP - 1) / GROUP, g0 = ng * wave / 4, g1 = ng * (wave + 1) / 4;
@@ -1274,6 +1312,7 @@ __device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias
                 const uint4 b = *at(32 * RB + (lane & 31), 2 * s + h);
 #pragma unroll
                 for (int i = 0; i < RB; ++i) {
+                    if (i > 0 && half) continue;
                     const uint4 a = *at(32 * i + (lane & 31), 2 * s + h);
                     if constexpr (sizeof(E) == 2) {
                         acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
@@ -1317,7 +1356,7 @@ struct FewStatsArgs {
     Saved s;
     const void* weight;
     float *mx, *sum, *sum_t;  // [strips][N]: a strip is a block's classes
-    int N, V, K, d, vpad;
+    int N, V, d, ldk;
     float scale, scale_t;
 };
 
@@ -1325,13 +1364,14 @@ template <typename E, int RB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3)))
 void few_stats_kernel(FewStatsArgs p) {
     __shared__ __attribute__((aligned(16))) char lds[FewLds<E, RB>::BYTES];
-    const int tid = threadIdx.x, n0 = blockIdx.x * kFewClasses, n = 1 + p.K;
-    // (all N places of rows, so that no load waits for the number of live ones; what is
-    // behind those is left out below. The first targets are requested ahead, too)
-    const int first = tid < p.N * n ? p.s.tidx[tid] : -1;
-    const int live = p.s.head->live;
-    few_z<E, RB>(static_cast<const E*>(p.s.x), static_cast<const E*>(p.weight), p.s.bias, p.N, p.V,
-                 p.d, n0, lds);
+    const int tid = threadIdx.x, n0 = blockIdx.x * kFewClasses;
+    const int r0 = blockIdx.y * kFewRows, rows = min(kFewRows, p.N - r0);
+    if (r0 > 0 && r0 >= p.s.head->live) return;
+    // (all places of rows, so that no load waits for the number of live ones: what is
+    // behind those is left out below)
+    const int live = min(rows, p.s.head->live - r0);
+    few_z<E, RB>(static_cast<const E*>(p.s.x) + static_cast<size_t>(r0) * p.d,
+                 static_cast<const E*>(p.weight), p.s.bias, rows, live, p.V, p.d, n0, lds);
     // four threads a row, eight classes each
     const int r = tid >> 2, c0 = 8 * (tid & 3);
     if (r < 32 * RB) {
@@ -1341,7 +1381,7 @@ void few_stats_kernel(FewStatsArgs p) {
             z[q] = few_at<E, RB>(lds, r)[c0 + q];
             m = fmaxf(m, z[q]);
         }
-        if (r < live) store8(p.s.z + static_cast<size_t>(r) * p.vpad + n0 + c0, z);
+        if (r < live) store8(p.s.z + static_cast<size_t>(r0 + r) * p.ldk + n0 + c0, z);
         m = fmaxf(m, __shfl_xor(m, 1, 64));
         m = fmaxf(m, __shfl_xor(m, 2, 64));
         auto total = [&](float scale) {
@@ -1354,38 +1394,31 @@ void few_stats_kernel(FewStatsArgs p) {
             return s + __shfl_xor(s, 2, 64);
         };
         const float s = total(p.scale), st = p.sum_t != nullptr ? total(p.scale_t) : 0.0f;
-        const size_t at = static_cast<size_t>(blockIdx.x) * p.N + r;
+        const size_t at = static_cast<size_t>(blockIdx.x) * p.N + r0 + r;
         if (r < live && (tid & 3) == 0) {
             p.mx[at] = m;
             p.sum[at] = s;
             if (p.sum_t != nullptr) p.sum_t[at] = st;
         }
     }
-    // the logits of the targets among these classes
-#pragma unroll 4
-    for (int e = tid; e < live * n; e += 256) {
-        const int c = e == tid ? first : p.s.tidx[e];
-        if (c >= n0 && c < n0 + kFewClasses) p.s.tz[e] = few_at<E, RB>(lds, e / n)[c - n0];
-        else if (c < 0 && blockIdx.x == 0) p.s.tz[e] = 0.0f;
-    }
 }
 
 struct FewGradArgs {
     Saved s;
     void* dz;
-    int first, cols, K, ldz, vpad;  // the piece's classes
+    int first, per, N, K, ldz, ldk;  // the piece's first class, its classes by eight
     int mean;
     float w_label, w_teacher, inv_t;
 };
 
-// dz from the z that was kept, eight classes a thread; blockIdx.y: the row.
+// dz from the z that was kept, eight classes a thread.
 template <typename E>
 __global__ __launch_bounds__(256) void few_grad_kernel(FewGradArgs p) {
-    const int r = blockIdx.y, c = 8 * (blockIdx.x * 256 + threadIdx.x);
+    const int i = blockIdx.x * 256 + threadIdx.x, r = i / p.per, c = 8 * (i - r * p.per);
     const Header h = *p.s.head;
-    if (r >= h.live || c >= p.cols) return;
+    if (r >= h.live) return;
     float v[8];
-    load8(p.s.z + static_cast<size_t>(r) * p.vpad + p.first + c, v);
+    load8(p.s.z + static_cast<size_t>(r) * p.ldk + p.first + c, v);
     const float4 rec = p.s.rec[r];
     const float2 g = Rates(h, p.w_label, p.w_teacher, p.mean).of(p.s.weight[r]);
     const Softmax soft(h, p.K > 0, p.inv_t);
@@ -1407,7 +1440,7 @@ struct FinishArgs {
     double* sums;  // [blocks][4]
     unsigned* ticket;
     float *losses, *row_losses;
-    int strips, N, K, mean;
+    int strips, N, K, mean, ldk;    // ldk: a row of the z that was kept, 0 where none was
     float temperature, inv, inv_t;  // inv: of `sum`'s softmax
 };
 
@@ -1456,6 +1489,13 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     const int lr = lane % LR, r = blockIdx.x * LR + lr;
     const bool in = r < live, two = p.sum_t != nullptr;
     const float scale = kLog2e * p.inv, scale_t = kLog2e * p.inv_t;
+    // The logit of target e of row r: where the tiles left it, or from the z that was kept
+    // (0 of one that is none).
+    auto target = [&](int r, size_t e) {
+        if (p.ldk == 0) return p.s.tz[e];
+        const int c = p.s.tidx[e];
+        return p.s.tz[e] = c >= 0 ? p.s.z[static_cast<size_t>(r) * p.ldk + c] : 0.0f;
+    };
     // (requested ahead of the strips)
     const bool owner = wave == 0 && lane < LR && in;
     float2 weight = make_float2(0.0f, 0.0f);
@@ -1465,7 +1505,7 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     if (owner) {
         weight = p.s.weight[r];
         rec = p.s.rec[r];
-        zlabel = p.s.tz[static_cast<size_t>(r) * (1 + p.K)];
+        zlabel = target(r, static_cast<size_t>(r) * (1 + p.K));
         row = p.s.row[r];
     }
     RowSums z;
@@ -1493,7 +1533,7 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
             const size_t entry = static_cast<size_t>(k) * (1 + p.K) + 1;
             float v = 0.0f;
             for (int j = lane; j < p.K; j += 64) {
-                const float q = p.s.tq[entry + j], zt = p.s.tz[entry + j] * p.inv_t;
+                const float q = p.s.tq[entry + j], zt = target(k, entry + j) * p.inv_t;
                 // (an entry without a share adds nothing, of a class masked out neither)
                 v = __builtin_fmaf(q, q == 0.0f ? 0.0f : zt, v);
             }
@@ -1839,7 +1879,7 @@ FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     p.tile_rows = s.dtype == VMOE_BF16 ? TileBig::BM : F32Tile::BM;
     p.tile_shift = s.dtype == VMOE_BF16 ? 8 : 7;
     p.tiles_n = static_cast<int>(cdiv(s.n_classes, 1 << p.tile_shift));
-    p.few = s.n_rows <= kFewRows;
+    p.few = few_logits(s);
     p.strips = p.few ? static_cast<int>(cdiv(s.n_classes, kFewClasses)) : 2 * p.tiles_n;
     // few rows: four lanes a row, since many strips stand before each
     p.finish_rows = s.n_rows <= 2048 ? 16 : 64;
@@ -1857,10 +1897,9 @@ FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     p.mx_off = take(4 * N * p.strips);
     p.sum_off = take(4 * N * p.strips);
     p.sumt_off = take(p.two ? 4 * N * p.strips : 0);
-    p.list_off = take(4 * N * s.n_teacher);
-    p.ends_off = take(s.n_teacher > 0 ? 4 * cdiv(s.n_rows, p.tile_rows) *
-                                            static_cast<size_t>(p.tiles_n)
-                                      : 0);
+    p.list_off = take(keeps_logits(s) ? 0 : 4 * N * s.n_teacher);
+    const size_t tiles_m = cdiv(s.n_rows, p.tile_rows);
+    p.ends_off = take(s.n_teacher > 0 && !keeps_logits(s) ? 4 * tiles_m * p.tiles_n : 0);
     p.bytes = c.off;
     return p;
 }
@@ -1928,27 +1967,32 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
     float* const sum = reinterpret_cast<float*>(base + p.sum_off);
     float* const sum_t = p.two ? reinterpret_cast<float*>(base + p.sumt_off) : nullptr;
     const float inv = K > 0 && labels == nullptr ? inv_t : 1.0f;  // of `sum`
-    if (p.few) {
+    if (N <= kFewRows) {
         const unsigned grid = row_grid + cdiv(zb.vpad, 256);
         if (bf16) rows_kernel<uint16_t, true><<<grid, 256, 0, st>>>(t);
         else rows_kernel<float, true><<<grid, 256, 0, st>>>(t);
-        const FewStatsArgs a{v, weight, mx, sum, sum_t, N, V, K, s.d_model, zb.vpad,
-                             kLog2e * inv, kLog2e * inv_t};
-        auto go = [&](auto blocks) {
-            constexpr int RB = decltype(blocks)::value;
-            if (bf16) few_stats_kernel<uint16_t, RB><<<p.strips, 256, 0, st>>>(a);
-            else few_stats_kernel<float, RB><<<p.strips, 256, 0, st>>>(a);
-        };
-        if (N > 32) go(std::integral_constant<int, 2>{});
-        else if (N > 0) go(std::integral_constant<int, 1>{});
     } else {
         mark_kernel<<<p.row_blocks + cdiv(zb.vpad, p.mark_rows), p.mark_rows, 0, st>>>(m);
         if (bf16) rows_kernel<uint16_t, false><<<row_grid, 256, 0, st>>>(t);
         else rows_kernel<float, false><<<row_grid, 256, 0, st>>>(t);
+    }
+    if (p.few) {
+        const FewStatsArgs a{v, weight, mx, sum, sum_t, N, V, s.d_model, kept_classes(s),
+                             kLog2e * inv, kLog2e * inv_t};
+        auto go = [&](auto blocks) {
+            constexpr int RB = decltype(blocks)::value;
+            const dim3 grid(p.strips, cdiv(N, kFewRows));
+            if (bf16) few_stats_kernel<uint16_t, RB><<<grid, 256, 0, st>>>(a);
+            else few_stats_kernel<float, RB><<<grid, 256, 0, st>>>(a);
+        };
+        if (N > 32) go(std::integral_constant<int, 2>{});
+        else if (N > 0) go(std::integral_constant<int, 1>{});
+    } else {
+        const bool sorted = K > 0 && !keeps_logits(s);
         const SortArgs g{v, reinterpret_cast<uint32_t*>(base + p.list_off),
                          reinterpret_cast<int32_t*>(base + p.ends_off), K, p.tile_rows,
                          p.tile_shift, p.tiles_n};
-        if (K > 0) sort_kernel<<<cdiv(N, p.tile_rows), 1024, 0, st>>>(g);
+        if (sorted) sort_kernel<<<cdiv(N, p.tile_rows), 1024, 0, st>>>(g);
         StatsArgs a{};
         a.a = Operand{v.x, 0, s.d_model};
         a.b = Operand{weight, 0, s.d_model};
@@ -1963,7 +2007,9 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
         a.sum_t = sum_t;
         a.tidx = v.tidx;
         a.tz = v.tz;
-        a.list = K > 0 ? g.list : nullptr;
+        a.list = sorted ? g.list : nullptr;
+        a.z = keeps_logits(s) ? v.z : nullptr;
+        a.ldk = kept_classes(s);
         a.ends = g.ends;
         a.n_rows = N;
         a.per_row = 1 + K;
@@ -1975,7 +2021,7 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
 
     const FinishArgs f{v, mx, sum, sum_t, reinterpret_cast<double*>(base + p.sums_off), zb.ticket,
                        losses, row_losses, p.strips, N, K, s.reduction == VMOE_REDUCE_MEAN,
-                       s.temperature, inv, inv_t};
+                       keeps_logits(s) ? kept_classes(s) : 0, s.temperature, inv, inv_t};
     if (p.finish_rows == 16) finish_kernel<16><<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
     else finish_kernel<64><<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
     return launch_status();
@@ -2018,12 +2064,12 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
         z.teacher = s.n_teacher > 0;
         z.label = z.teacher ? nullptr : v.tidx;
         z.first = first;
-        if (N <= kFewRows) {
+        if (keeps_logits(s)) {
             // (the forward wrote z of whole blocks of classes)
-            const int cols = static_cast<int>(cdiv(count, kFewClasses)) * kFewClasses;
-            const FewGradArgs u{v, z.dz, first, cols, s.n_teacher, z.ldz, padded_classes(s),
+            const int per = static_cast<int>(cdiv(count, kFewClasses)) * kFewClasses / 8;
+            const FewGradArgs u{v, z.dz, first, per, N, s.n_teacher, z.ldz, kept_classes(s),
                                 z.mean, z.w_label, z.w_teacher, z.inv_t};
-            const dim3 grid(cdiv(cols, 2048), N);
+            const unsigned grid = cdiv(static_cast<long long>(N) * per, 256);
             if (N > 0 && bf16) few_grad_kernel<uint16_t><<<grid, 256, 0, st>>>(u);
             else if (N > 0) few_grad_kernel<float><<<grid, 256, 0, st>>>(u);
         } else {

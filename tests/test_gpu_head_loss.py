@@ -70,6 +70,35 @@ CASES = {
     "many_classes_few_rows": Case(3, 64, 30001, k=8, t=2.0),
     "many_rows_few_classes": Case(9000, 64, 17),
     "many_rows_few_classes_f32": Case(9000, 64, 17, dtype="f32"),
+    # more logits than the kernels of few take: tiles, and z formed twice
+    "tiles_below": Case(1279, 72, 3583, ignored=0.2),
+    "tiles_even": Case(1280, 64, 3584, weighted=True),
+    "tiles_above": Case(1281, 192, 3585, k=5, t=2.0),
+    "tiles_odd": Case(1300, 128, 4003, k=17, t=2.0, ignored=0.4, missing=0.3, weighted=True),
+    "tiles_no_bias": Case(1100, 96, 4100, bias=False),
+    "tiles_teacher_alone": Case(1290, 64, 3841, k=64, t=1.5, labels=False),
+    "tiles_teacher_alone_t1": Case(1290, 64, 3841, k=63, labels=False, missing=0.9),
+    "tiles_teacher_t1": Case(1300, 320, 3700, k=65),
+    "tiles_longest_list": Case(1281, 64, 3999, k=256, t=2.0, missing=0.2),
+    "tiles_nearly_all_out": Case(2100, 64, 3000, k=3, ignored=0.995),
+    "tiles_all_out": Case(1300, 64, 4000, k=4, ignored=1.0),
+    "tiles_summed": Case(1200, 64, 4000, k=4, t=2.0, reduction=H.VMOE_REDUCE_SUM, weighted=True,
+                         ignored=0.1),
+    "tiles_one_class": Case(131100, 8, 1, k=1, t=3.0),
+    "tiles_few_classes_t0.7": Case(131100, 16, 10, k=2, t=0.7),
+    "tiles_few_classes_t5.3_f32": Case(50000, 16, 10, k=2, t=5.3, dtype="f32"),
+    "tiles_below_f32": Case(1087, 40, 1663, dtype="f32", ignored=0.1),
+    "tiles_odd_f32": Case(1000, 136, 2003, k=17, t=2.0, dtype="f32", ignored=0.4, missing=0.3,
+                          weighted=True),
+    "tiles_longest_list_f32": Case(1000, 64, 2003, k=256, t=2.0, dtype="f32", labels=False),
+    "tiles_all_out_f32": Case(1000, 64, 2003, k=4, dtype="f32", ignored=1.0),
+    # f32 tiles whose z is kept
+    "kept_f32": Case(1088, 192, 1664, dtype="f32", weighted=True),
+    "kept_odd_f32": Case(1000, 200, 2003, k=17, t=2.0, dtype="f32", ignored=0.4, missing=0.3,
+                         weighted=True),
+    "kept_teacher_alone_f32": Case(1089, 256, 1665, k=100, t=3.0, dtype="f32", labels=False,
+                                   bias=False),
+    "kept_all_out_f32": Case(1000, 200, 2003, k=4, dtype="f32", ignored=1.0),
     "narrow_tiles": Case(600, 192, 4000, k=2),
     "long": Case(5000, 256, 5001, weighted=True, ignored=0.1),
 }
@@ -159,14 +188,15 @@ def test_weights_of_the_losses(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n, reduction", [(40, 0), (300, 0), (300, 1)])
-def test_rows_of_negative_weight(dtype, n, reduction):
-    c = Case(n, 64, 200, k=3, t=2.0, dtype=dtype, reduction=reduction)
+@pytest.mark.parametrize("n, v, reduction", [(40, 200, 0), (300, 200, 0), (300, 200, 1),
+                                             (1300, 4000, 0), (1300, 4000, 1)])
+def test_rows_of_negative_weight(dtype, n, v, reduction):
+    c = Case(n, 64, v, k=3, t=2.0, dtype=dtype, reduction=reduction)
     d = Data(c)
     g = torch.Generator(device="cuda").manual_seed(9)
     d.row_weight = torch.randn(n, device="cuda", generator=g) + 0.5
     check(c, d)
-    label = Data(Case(n, 64, 200, dtype=dtype, reduction=reduction))
+    label = Data(Case(n, 64, v, dtype=dtype, reduction=reduction))
     label.row_weight = d.row_weight
     check(label.case, label)
 
@@ -182,9 +212,10 @@ def test_the_weight_of_a_loss_that_is_not_there(dtype):
             assert same_bits(a[k], b[k]), k
 
 
-def test_weights_beyond_2_gib():
+@pytest.mark.parametrize("n", [40, 70])
+def test_weights_beyond_2_gib(n):
     """Offsets past 32 bits in the head's weight and its gradient, and several pieces."""
-    n, d, v = 70, 1024, 1100003
+    d, v = 1024, 1100003
     assert v * d * 2 > 2 ** 31
     c = Case(n, d, v, k=2, t=2.0, bias=False)
     data = Data(c)
@@ -199,8 +230,10 @@ def test_weights_beyond_2_gib():
     torch.cuda.empty_cache()
 
 
-def test_several_backwards_of_one_forward():
-    d = Data(Case(90, 64, 200, k=6, t=2.0))
+@pytest.mark.parametrize("c", [Case(90, 64, 200, k=6, t=2.0), Case(1300, 64, 4000, k=6, t=2.0),
+                               Case(1000, 192, 2003, k=6, t=2.0, dtype="f32")])
+def test_several_backwards_of_one_forward(c):
+    d = Data(c)
     s = d.case.shape()
     first = d.run()
     before = d.saved.clone()
@@ -214,7 +247,8 @@ def test_several_backwards_of_one_forward():
 
 
 @pytest.mark.parametrize("name", ["odd_classes", "odd_classes_f32", "long", "mark_blocks",
-                                  "many_rows_few_classes"])
+                                  "many_rows_few_classes", "tiles_odd", "tiles_odd_f32",
+                                  "kept_odd_f32"])
 def test_same_bits_every_time(name):
     d = Data(CASES[name])
     a, b = d.run(), d.run(spoil=False)
@@ -267,7 +301,7 @@ def test_weights_that_cancel(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n", [40, 200])
+@pytest.mark.parametrize("n", [40, 200, 6400])
 @pytest.mark.parametrize("t", [1.0, 1.7])
 @pytest.mark.parametrize("lowest", [False, True])
 def test_classes_masked_by_the_bias(dtype, n, t, lowest):
@@ -306,9 +340,10 @@ def test_classes_masked_by_the_bias(dtype, n, t, lowest):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("shift", [-300.0, 300.0])
-def test_large_logits(dtype, shift):
+@pytest.mark.parametrize("n, v", [(70, 130), (1300, 4000)])
+def test_large_logits(dtype, shift, n, v):
     """Logits far from 0 and rows that are certain."""
-    c = Case(70, 64, 130, k=4, t=2.0, dtype=dtype)
+    c = Case(n, 64, v, k=4, t=2.0, dtype=dtype)
     d = Data(c)
     d.bias = (d.bias.float() + shift).to(d.bias.dtype)
     d.x = (4 * d.x.float()).to(d.x.dtype)
@@ -337,13 +372,13 @@ def test_on_another_stream_and_handle():
 
 def test_streams_side_by_side():
     """Two heads at once, each with its own buffers."""
-    ds = [Data(CASES["odd_classes"]), Data(CASES["tile_edge_above"])]
+    ds = [Data(CASES[k]) for k in ("odd_classes", "tile_edge_above", "tiles_odd", "kept_odd_f32")]
     want = [d.run() for d in ds]
     streams = [torch.cuda.Stream() for _ in ds]
     out = []
     for d, st in zip(ds, streams):
         c, s = d.case, d.case.shape()
-        new = lambda *sh, dt=torch.bfloat16: torch.empty(*sh, dtype=dt, device="cuda")  # noqa: E731
+        new = lambda *sh, dt=d.x.dtype: torch.empty(*sh, dtype=dt, device="cuda")  # noqa: E731
         u8 = lambda k: new(max(k, 16), dt=torch.uint8)  # noqa: E731
         o = dict(losses=new(4, dt=torch.float32), row_losses=new(c.n, 2, dt=torch.float32),
                  dx=new(c.n, c.d), dweight=new(c.v, c.d), dbias=new(c.v))
@@ -363,11 +398,13 @@ def test_streams_side_by_side():
             assert same_bits(o[k], w[k]), k
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_captured_and_replayed(dtype):
+@pytest.mark.parametrize("dtype, n, d_model, v", [
+    ("bf16", 400, 64, 600), ("f32", 400, 64, 600), ("bf16", 1300, 64, 4000),
+    ("f32", 1000, 64, 2003), ("f32", 1000, 192, 2003)])
+def test_captured_and_replayed(dtype, n, d_model, v):
     """One graph of forward and backward, replayed on other inputs (another number of
     live rows among them), with eager work in between."""
-    c = Case(400, 64, 600, k=4, t=2.0, dtype=dtype, ignored=0.3, weighted=True)
+    c = Case(n, d_model, v, k=4, t=2.0, dtype=dtype, ignored=0.3, weighted=True)
     s, act = c.shape(), torch.bfloat16 if dtype == "bf16" else torch.float32
     d = Data(c)
     new = lambda *sh, dt=act: torch.empty(*sh, dtype=dt, device="cuda")  # noqa: E731
@@ -388,7 +425,7 @@ def test_captured_and_replayed(dtype):
     with torch.cuda.graph(graph):
         step()
     for k, ignored in enumerate((0.3, 0.9, 0.0, 1.0, 0.5)):
-        e = Data(Case(400, 64, 600, k=4, t=2.0, dtype=dtype, ignored=ignored, weighted=True,
+        e = Data(Case(n, d_model, v, k=4, t=2.0, dtype=dtype, ignored=ignored, weighted=True,
                       seed=10 + k))
         for a in ("x", "weight", "bias", "labels", "idx", "logits", "row_weight"):
             getattr(d, a).copy_(getattr(e, a))
