@@ -16,7 +16,8 @@
 //   grad_z    z by tiles, or as it was kept -> dz, in the operands' type
 //   subtract  with a teacher, dz at the targets, in f32 from their logits, rounded once
 //   products  dx += dz W (f32 partial sums in slots), dW = dz^T x, db = sums of dz
-// and in the end dx from the slots, rounded once, rows back to their places.
+// and in the end dx from the slots, rounded once, rows back to their places (where one
+// block has all of k, the product writes them itself).
 // Only live rows reach the products: their number is read on the device, tiles past
 // it end at once, so padding costs nothing and the host waits for nothing.
 //
@@ -206,6 +207,17 @@ struct PartArgs : Product {
     static constexpr bool A_KMAJOR = LEFT, B_KMAJOR = false;
 };
 
+struct DxArgs : Product {  // dz times the weight, rounded, k in one range
+    void* dx;             // [.., N], rows by their numbers
+    const int32_t* row;   // [M]
+    const float* before;  // [M, N] sums of the pieces before, or null
+    const Header* head;
+    float w_label, w_teacher;
+    int mean;
+    static constexpr int OUT = EPI_F32;
+    static constexpr bool A_KMAJOR = true, B_KMAJOR = false;
+};
+
 struct StoreArgs : Product {  // dz^T times x, rounded, k in one range
     void* c;      // [M, N], or null
     void* sums;   // [M] of A's rows, or null
@@ -318,12 +330,16 @@ struct Ahead<T, GradZArgs> {
 template <class T>
 struct Ahead<T, StoreArgs> {
     float all;
-    __device__ __forceinline__ void load(const StoreArgs& p, int, int, int) {
+    template <class ARGS>
+    __device__ __forceinline__ void load(const ARGS& p, int, int, int) {
         const float f = Rates(*p.head, p.w_label, p.w_teacher, p.mean).all;
         all = __builtin_bit_cast(
             float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
     }
 };
+
+template <class T>
+struct Ahead<T, DxArgs> : Ahead<T, StoreArgs> {};
 
 // Block b runs on XCD b mod 8; XCDs take chunks of neighbouring tiles in turn, and
 // tiles go in groups of group_m rows of tiles, so that an XCD's blocks share operand
@@ -613,15 +629,19 @@ __device__ __forceinline__ lds_u16* wave_lds(const LdsArrays& arrays) {
     return (lds_u16*)(arrays.b6) + wave_id() * 2048;
 }
 
+struct InOrder {
+    __device__ __forceinline__ int operator()(int r) const { return r; }
+};
+
 // One 32 x 32 block of a wave's outputs to rows of `dst` (element type E), through LDS
 // of the wave's own: rows leave as 16-byte pieces, eight (f32) or four lanes a row.
 // Row r of the block goes to dst + r ld; rows from `rows` and columns from `cols`
 // (a multiple of 8 unless the row is padded beyond it) are left out; `flip` (bf16): a
-// mask over two rounded values, for their signs. A wave's LDS accesses run in order: no
-// barrier.
-template <typename E>
+// mask over two rounded values, for their signs; `row`: which row of dst r stands for. A
+// wave's LDS accesses run in order: no barrier.
+template <typename E, class ROW = InOrder>
 __device__ __forceinline__ void store_block(const f32x16& v, lds_u16* s, E* dst, size_t ld,
-                                            int rows, int cols, uint32_t flip = 0) {
+                                            int rows, int cols, uint32_t flip = 0, ROW row = {}) {
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     if constexpr (sizeof(E) == 4) {
         put_block(v, s);
@@ -629,7 +649,8 @@ __device__ __forceinline__ void store_block(const f32x16& v, lds_u16* s, E* dst,
         for (int u = 0; u < 4; ++u) {
             const int rr = 8 * u + (lane >> 3), c = lane & 7;
             const v4i32 w = *reinterpret_cast<lds_v4*>(s + rr * 64 + ((c ^ (rr & 7)) << 3));
-            if (rr < rows && 4 * c < cols) *reinterpret_cast<v4i32*>(dst + rr * ld + 4 * c) = w;
+            if (rr < rows && 4 * c < cols)
+                *reinterpret_cast<v4i32*>(dst + row(rr) * ld + 4 * c) = w;
         }
     } else {
         typedef int v2i32 __attribute__((ext_vector_type(2)));
@@ -644,7 +665,8 @@ __device__ __forceinline__ void store_block(const f32x16& v, lds_u16* s, E* dst,
             const int rr = 16 * u + (lane >> 2), c = lane & 3;
             const v4i32 w =
                 *reinterpret_cast<lds_v4*>(s + rr * 32 + ((c ^ ((rr >> 2) & 3)) << 3));
-            if (rr < rows && 8 * c < cols) *reinterpret_cast<v4i32*>(dst + rr * ld + 8 * c) = w;
+            if (rr < rows && 8 * c < cols)
+                *reinterpret_cast<v4i32*>(dst + row(rr) * ld + 8 * c) = w;
         }
     }
 }
@@ -817,6 +839,24 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, Gra
     }
 }
 
+// v += the 32 x 32 block at `at`, whose rows are `ld` long and of which `rows` and `cols`
+// are left.
+__device__ __forceinline__ void add_block(f32x16& v, const float* at, size_t ld, int rows,
+                                          int cols) {
+    const int lane = threadIdx.x & 63, r = lane & 31;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int c = 8 * q + 4 * (lane >> 5);
+        if (r < rows && c < cols) {
+            const float4 o = *reinterpret_cast<const float4*>(at + r * ld + c);
+            v[4 * q] += o.x;
+            v[4 * q + 1] += o.y;
+            v[4 * q + 2] += o.z;
+            v[4 * q + 3] += o.w;
+        }
+    }
+}
+
 // f32 sums of the tile's range of k, into its slot.
 template <class T, int EPI, bool LEFT>
 __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, PartArgs<LEFT>>& p,
@@ -841,22 +881,38 @@ __device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, Par
             if (n >= N) break;
             float* const at = part + static_cast<size_t>(p.t_m0 + r0) * p.N + p.t_n0 + n;
             f32x16 v = acc[i][b];
-            if (p.add) {
-                const int r = lane & 31;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int c = 8 * q + 4 * (lane >> 5);
-                    if (r0 + r < M && n + c < N) {
-                        const float4 o = *reinterpret_cast<const float4*>(
-                            at + static_cast<size_t>(r) * p.N + c);
-                        v[4 * q] += o.x;
-                        v[4 * q + 1] += o.y;
-                        v[4 * q + 2] += o.z;
-                        v[4 * q + 3] += o.w;
-                    }
-                }
-            }
+            if (p.add) add_block(v, at, p.N, M - r0, N - n);
             store_block(v, wave_lds(arrays), at, p.N, M - r0, N - n);
+        }
+    }
+}
+
+// dx itself, where one block has all of k: 28066 x 2632 rows against 170 classes
+// 455 -> 348 us, of which f32 sums, their rounding and its launch took 110.
+template <class T, int EPI>
+__device__ __forceinline__ void finish_tile(TileKind<T, EPI>, const Tiled<T, DxArgs>& p,
+                                            f32x16 (&acc)[T::FM][T::PB], float (&)[T::FM], bool,
+                                            const LdsArrays& arrays, int, int M, int N, int, int,
+                                            int fm_live) {
+    const int wave = wave_id(), wm = wave / T::WGN, wn = wave % T::WGN;
+    const float all = p.ahead.all;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+        if (i >= fm_live) break;
+        const int r0 = T::WM * wm + 32 * i;
+        const int32_t* const row = p.row + p.t_m0 + r0;
+#pragma unroll
+        for (int b = 0; b < T::PB; ++b) {
+            const int n = 64 * b + 32 * wn;
+            if (n >= N) break;
+            f32x16 v = acc[i][b];
+            if (p.before != nullptr)
+                add_block(v, p.before + static_cast<size_t>(p.t_m0 + r0) * p.N + p.t_n0 + n, p.N,
+                          M - r0, N - n);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) v[q] *= all;
+            store_block(v, wave_lds(arrays), static_cast<Elm<T>*>(p.dx) + p.t_n0 + n, p.N, M - r0,
+                        N - n, 0, [row](int r) { return row[r]; });
         }
     }
 }
@@ -1739,6 +1795,18 @@ __global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ part,
     if (in) store8(dx + static_cast<size_t>(t) * d + c, v);
 }
 
+// dx of rows that were left out, a wave a row, where the products write the others'.
+template <typename E>
+__global__ __launch_bounds__(256) void zero_kernel(const int32_t* __restrict__ place,
+                                                   E* __restrict__ dx, int N, int d) {
+    const int t = blockIdx.x * 4 + wave_id();
+    if (t >= N || place[t] >= 0) return;
+    constexpr int PER = 16 / sizeof(E);
+    E* const out = dx + static_cast<size_t>(t) * d;
+    for (int c = PER * (threadIdx.x & 63); c < d; c += 64 * PER)
+        *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
+}
+
 // dW and db of a piece from the slots of its ranges of rows.
 template <typename E>
 __global__ __launch_bounds__(256) void dw_kernel(const float* __restrict__ part, size_t stride,
@@ -1816,7 +1884,8 @@ Cut choose_cut(const vmoe_head_shape& s, long long cols) {
             for (const int w : ranges) {
                 if (w > 1 && (w > sw || w > 16 || tw * w > 4 * cus)) break;
                 const double time_w = stage * ((sw + w - 1) / w + extra);
-                double c = ends_at(cus, tx * x, time_x, tw * w, time_w) + part * tx * x;
+                double c = ends_at(cus, tx * x, time_x, tw * w, time_w);
+                if (x > 1) c += part * tx * x;
                 if (w > 1) c += part * tw * w + 3.0;  // and a launch
                 if (c < least) {
                     least = c;
@@ -1854,7 +1923,7 @@ Plan make_plan(const vmoe_head_shape& s) {
         return at;
     };
     p.dz_off = take(static_cast<size_t>(N) * p.cols * elem_bytes(s));
-    p.dx_off = take(4 * static_cast<size_t>(p.cut.dx) * N * d);
+    p.dx_off = take(p.cut.dx > 1 || p.pieces > 1 ? 4 * static_cast<size_t>(p.cut.dx) * N * d : 0);
     p.dw_off = take(p.cut.dw > 1 ? 4 * static_cast<size_t>(p.cut.dw) * p.cols * d : 0);
     p.sums_off = take(p.cut.dw > 1 ? 4 * static_cast<size_t>(p.cut.dw) * p.cols : 0);
     p.bytes = c.off;
@@ -2114,7 +2183,18 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
         char* const dbp = dbias != nullptr
                               ? static_cast<char*>(dbias) + static_cast<size_t>(first) * size
                               : nullptr;
+        const bool last = (i + 1) * static_cast<long long>(p.cols) >= V;
+        const bool finish_dx = p.cut.dx == 1 && last;
         const long long rows_l = dx != nullptr ? N : 0;
+        DxArgs o{};
+        static_cast<Product&>(o) = l;
+        o.dx = dx;
+        o.row = v.row;
+        o.before = i > 0 ? l.part : nullptr;
+        o.head = v.head;
+        o.w_label = factor.w_label;
+        o.w_teacher = factor.w_teacher;
+        o.mean = factor.mean;
         const long long rows_r = dweight != nullptr || dbias != nullptr ? count : 0;
         if (r.splits == 1) {
             StoreArgs c{};
@@ -2126,7 +2206,8 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             c.w_label = factor.w_label;
             c.w_teacher = factor.w_teacher;
             c.mean = factor.mean;
-            launch_products(s, p.cut.narrow, l, rows_l, c, rows_r, st);
+            if (finish_dx) launch_products(s, p.cut.narrow, o, rows_l, c, rows_r, st);
+            else launch_products(s, p.cut.narrow, l, rows_l, c, rows_r, st);
         } else {
             PartArgs<false> c{};
             static_cast<Product&>(c) = r;
@@ -2134,7 +2215,8 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             c.part_stride = static_cast<size_t>(count) * d;
             c.part_sums = dbp != nullptr ? reinterpret_cast<float*>(base + p.sums_off) : nullptr;
             c.bsum = c.part_sums;
-            launch_products(s, p.cut.narrow, l, rows_l, c, rows_r, st);
+            if (finish_dx) launch_products(s, p.cut.narrow, o, rows_l, c, rows_r, st);
+            else launch_products(s, p.cut.narrow, l, rows_l, c, rows_r, st);
             const unsigned grid = cdiv(static_cast<long long>(count) * (d / 8), 256);
             if (bf16)
                 dw_kernel<<<grid, 256, 0, st>>>(c.part, c.part_stride, c.part_sums, r.splits,
@@ -2146,7 +2228,11 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
                                                 reinterpret_cast<float*>(dbp), count, d, factor);
         }
     }
-    if (dx != nullptr && N > 0) {
+    if (dx != nullptr && N > 0 && p.cut.dx == 1) {
+        const unsigned grid = cdiv(N, 4);
+        if (bf16) zero_kernel<<<grid, 256, 0, st>>>(v.place, static_cast<uint16_t*>(dx), N, d);
+        else zero_kernel<<<grid, 256, 0, st>>>(v.place, static_cast<float*>(dx), N, d);
+    } else if (dx != nullptr && N > 0) {
         const float* const part = reinterpret_cast<const float*>(base + p.dx_off);
         const size_t stride = static_cast<size_t>(N) * d;
         auto go = [&](auto groups) {
