@@ -64,7 +64,7 @@ struct Saved {
     float4* rec;     // [N] max z, log2 of the sums of exp(z - max) and of its T-th root,
                      //     sum_j q_j log q_j
     float2* weight;  // [N] weights in the two losses
-    float* bias;     // [V up to 256] f32, -infinity from V on
+    float* bias;     // [V up to 256, and 256] f32, -infinity from V on
     int32_t* tidx;   // [N, 1 + K] the label and the entries' classes, -1 without
     float* tz;       // [N, 1 + K] their logits
     float* tq;       // [N, 1 + K] 1 and q
@@ -100,6 +100,8 @@ bool keeps_logits(const vmoe_head_shape& s) {
 }
 
 int padded_classes(const vmoe_head_shape& s) { return static_cast<int>(up256(s.n_classes)); }
+// The bias's: tiles of 192 classes may end 191 behind the last.
+int padded_bias(const vmoe_head_shape& s) { return padded_classes(s) + 256; }
 size_t elem_bytes(const vmoe_head_shape& s) { return s.dtype == VMOE_BF16 ? 2 : 4; }
 
 struct Carver {
@@ -122,7 +124,7 @@ Saved saved_layout(const vmoe_head_shape& s, void* base) {
     v.place = c.take<int32_t>(N);
     v.rec = c.take<float4>(N);
     v.weight = c.take<float2>(N);
-    v.bias = c.take<float>(padded_classes(s));
+    v.bias = c.take<float>(padded_bias(s));
     v.tidx = c.take<int32_t>(E);
     v.tz = c.take<float>(E);
     v.tq = c.take<float>(E);
@@ -167,7 +169,7 @@ struct Product : GemmArgs {
 };
 
 struct StatsArgs : Product {
-    const float* zbias;       // [V up to 256]
+    const float* zbias;       // Saved::bias
     float *mx, *sum, *sum_t;  // [strips][N]
     const int32_t* tidx;      // [N, per_row]: the rows' labels first
     float* tz;                // and where their logits go, and the entries'
@@ -1942,12 +1944,28 @@ Plan make_plan(const vmoe_head_shape& s) {
     return p;
 }
 
+// Whether z takes 256 x 192 tiles in bf16: where the larger ones leave the last round of
+// CUs so empty that their rounds (stages, and the time of four for start and outputs) cost
+// 7 % more. Forward and backward of 7000 x 512 against 3000 classes 164 us with 256 x 256,
+// 151 so; 2048 x 1024 against 10 000 241, 224; 4661 x 112 against 3469 101, 93; where the
+// difference is less they cost more (2047 x 4096 against 65 537: 3.52 ms, 3.56).
+bool narrow_logits(const vmoe_head_shape& s, long long classes) {
+    if (s.dtype != VMOE_BF16) return false;
+    auto time = [&](int width, double stage) {
+        const long long tiles = static_cast<long long>(cdiv(s.n_rows, 256)) *
+                                ((classes + width - 1) / width);
+        return static_cast<double>((tiles + kCus - 1) / kCus) *
+               (stage * ((s.d_model + 63) / 64) + 4.0 * width / 256);
+    };
+    return time(192, 0.75 * 1.05) < 0.93 * time(256, 1.0);
+}
+
 static_assert(TileBig::BN == 256 && TileBig::WGN == 2 && F32Tile::BN == 128 && F32Tile::WGN == 2,
               "two strips a tile of z");
 
 struct FwdPlan {
     int few, mark_rows, row_blocks, strips, finish_rows, finish_blocks, two;
-    int tile_rows, tile_shift, tiles_n;  // of z
+    int tile_rows, tile_shift, tiles_n, narrow;  // of z
     size_t counts_off, ticket_off, sums_off, mx_off, sum_off, sumt_off, list_off, ends_off, bytes;
 };
 
@@ -1959,7 +1977,9 @@ FwdPlan make_fwd_plan(const vmoe_head_shape& s, bool labels) {
     p.row_blocks = static_cast<int>(cdiv(s.n_rows, p.mark_rows));
     p.tile_rows = s.dtype == VMOE_BF16 ? TileBig::BM : F32Tile::BM;
     p.tile_shift = s.dtype == VMOE_BF16 ? 8 : 7;
-    p.tiles_n = static_cast<int>(cdiv(s.n_classes, 1 << p.tile_shift));
+    // (entries are sorted by tiles whose width is a power of two)
+    p.narrow = s.n_teacher == 0 && narrow_logits(s, s.n_classes);
+    p.tiles_n = static_cast<int>(cdiv(s.n_classes, p.narrow ? TileNarrow::BN : 1 << p.tile_shift));
     p.few = few_logits(s);
     p.strips = p.few ? static_cast<int>(cdiv(s.n_classes, kFewClasses)) : 2 * p.tiles_n;
     // few rows: four lanes a row, since many strips stand before each
@@ -2013,11 +2033,10 @@ void launch_products(const vmoe_head_shape& s, int narrow, const FIRST& a, long 
     else launch_products<TileBig>(a, rows_a, b, rows_b, st);
 }
 
-// z, whose strips are those of 256 x 256 tiles.
+// z
 template <class ARGS>
-void launch_logits(const vmoe_head_shape& s, const ARGS& a, hipStream_t st) {
-    if (s.dtype != VMOE_BF16) launch_products<F32Tile>(a, a.M, NoProduct{}, 0, st);
-    else launch_products<TileBig>(a, a.M, NoProduct{}, 0, st);
+void launch_logits(const vmoe_head_shape& s, int narrow, const ARGS& a, hipStream_t st) {
+    launch_products(s, narrow, a, a.M, NoProduct{}, 0, st);
 }
 
 }  // namespace
@@ -2036,7 +2055,7 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
     const int N = s.n_rows, V = s.n_classes, K = s.n_teacher;
     const Told told{labels, teacher_idx, teacher_logits, row_weight, N, V, K};
     const BiasArgs zb{bias, v.bias, reinterpret_cast<unsigned*>(base + p.ticket_off), V,
-                      padded_classes(s), s.dtype == VMOE_BF16};
+                      padded_bias(s), s.dtype == VMOE_BF16};
     const MarkArgs m{told, zb, row_losses, v.place,
                      reinterpret_cast<int32_t*>(base + p.counts_off), p.row_blocks};
     const bool bf16 = s.dtype == VMOE_BF16;
@@ -2097,7 +2116,7 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
         a.has_bias = bias != nullptr;
         a.scale_t = kLog2e * inv_t;
         a.scale = kLog2e * inv;
-        launch_logits(s, a, st);
+        launch_logits(s, p.narrow, a, st);
     }
 
     const FinishArgs f{v, mx, sum, sum_t, reinterpret_cast<double*>(base + p.sums_off), zb.ticket,
@@ -2154,7 +2173,7 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             if (N > 0 && bf16) few_grad_kernel<uint16_t><<<grid, 256, 0, st>>>(u);
             else if (N > 0) few_grad_kernel<float><<<grid, 256, 0, st>>>(u);
         } else {
-            launch_logits(s, z, st);
+            launch_logits(s, narrow_logits(s, count), z, st);
         }
         if (N > 0 && z.teacher) {
             const SubtractArgs u{v, z.dz, z.ldz, first, count, s.n_teacher, z.mean, z.teacher,

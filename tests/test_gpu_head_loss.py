@@ -73,6 +73,7 @@ CASES = {
     # more logits than the kernels of few take: tiles, and z formed twice
     "tiles_below": Case(1279, 72, 3583, ignored=0.2),
     "tiles_even": Case(1280, 64, 3584, weighted=True),
+    "tiles_even_taught": Case(1280, 64, 3584, k=3, t=2.0),
     "tiles_above": Case(1281, 192, 3585, k=5, t=2.0),
     "tiles_odd": Case(1300, 128, 4003, k=17, t=2.0, ignored=0.4, missing=0.3, weighted=True),
     "tiles_no_bias": Case(1100, 96, 4100, bias=False),
