@@ -193,6 +193,19 @@ def test_weights_of_the_losses(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n, v", [(40, 200), (300, 200), (1300, 4000)])
+@pytest.mark.parametrize("w1, w2", [(0.5, -0.5), (-1.0, 0.25), (0.0, 1.0), (0.0, 0.0)])
+@pytest.mark.parametrize("temperature", [1.0, 2.0])
+def test_signs_of_the_losses(dtype, n, v, w1, w2, temperature):
+    """At temperature 1 with opposite weights the two softmaxes cancel, the targets stay."""
+    d = Data(Case(n, 64, v, k=3, t=temperature, dtype=dtype, weighted=True, ignored=0.2))
+    got = d.run(w1=w1, w2=w2)
+    ref, bound = d.reference(w1, w2)
+    for k in got:
+        close(k, got[k], ref[k], bound[k])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n, v, reduction", [(40, 200, 0), (300, 200, 0), (300, 200, 1),
                                              (1300, 4000, 0), (1300, 4000, 1)])
 def test_rows_of_negative_weight(dtype, n, v, reduction):

@@ -202,3 +202,14 @@ def test_options_of_the_block_refused(options):
                           capacity_factor=1.0)
     with pytest.raises(ValueError, match="^classes, teacher_top: "):
         SparseBlock(cfg, {}, **options)
+
+
+@pytest.mark.parametrize("options", [["--teacher-top", "5"], ["--classes", "-1"],
+                                     ["--classes", "4", "--teacher-top", "5"],
+                                     ["--classes", "1000", "--teacher-top", "257"]])
+def test_options_of_the_command_refused(options, monkeypatch, capsys):
+    from paper_2608_16188_amd import block
+    monkeypatch.setattr("sys.argv", ["block", *options])
+    with pytest.raises(SystemExit) as e:
+        block.main()
+    assert e.value.code == 2 and "--teacher-top" in capsys.readouterr().err
