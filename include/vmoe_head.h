@@ -64,8 +64,8 @@ size_t vmoe_head_loss_bwd_workspace_bytes(const vmoe_head_shape* shape);
  *   losses [4] f32 out; row_losses [N, 2] f32 out or NULL: a_t, b_t (0 without)
  *   saved: vmoe_head_loss_saved_bytes(shape) bytes out, for the backward
  * labels or a teacher has to be given. Rows with neither, or whose weight is 0, are
- * left out: their rows of x, and their teacher_logits, are not read and may hold
- * anything, and so may the logits of entries without a class. Such rows cost nothing
+ * left out: whatever their rows of x and their teacher_logits hold, NaN too, moves
+ * nothing, and neither do the logits of entries without a class. Such rows cost nothing
  * in the products. bf16 products run on matrix cores with f32 accumulation, f32
  * ones in f32; lse, q and losses are f32, sums over rows double. */
 vmoe_status vmoe_head_loss_fwd(const vmoe_head_shape* shape, const void* x, const void* weight,

@@ -1098,7 +1098,7 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
 struct RowArgs {
     const void* x;
     Told told;
-    BiasArgs bias;  // FEW
+    unsigned* ticket;  // FEW
     float* row_losses;
     const int32_t* counts;
     Saved s;
@@ -1107,21 +1107,17 @@ struct RowArgs {
 };
 
 // Rows 4 b .. + 3 of block b, a wave each. FEW (at most 64 rows): every wave marks all
-// of them itself, so that no launch stands before, and blocks behind the rows' take
-// the bias. Bound by the copy of x: 27 696 rows of 1024 in bf16 28 us, 4.3 TB/s.
+// of them itself, so that no launch stands before. Bound by the copy of x: 27 696 rows of
+// 1024 in bf16 28 us, 4.3 TB/s.
 template <typename E, bool FEW>
-__global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
+__device__ __forceinline__ void place_rows(const RowArgs& p) {
     constexpr int R = (VMOE_HEAD_MAX_TEACHER + 63) / 64;  // entries a lane
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int t = blockIdx.x * 4 + wave, mine = blockIdx.x * 4 / p.mark_rows;
     const int V = p.told.V, K = p.told.K;
     uint64_t marks = 0;
     if constexpr (FEW) {
-        const int row_blocks = max(1, (p.told.N + 3) / 4);
-        if (static_cast<int>(blockIdx.x) >= row_blocks) {
-            pad_bias(p.bias, (blockIdx.x - row_blocks) * 256 + threadIdx.x);
-            return;
-        }
+        if (blockIdx.x == 0 && threadIdx.x == 0) *p.ticket = 0;
         marks = __ballot(row_is_live(p.told, 0));
     }
     auto live_before = [&](int blocks) {
@@ -1226,6 +1222,9 @@ __global__ __launch_bounds__(256) void rows_kernel(RowArgs p) {
     }
 }
 
+template <typename E>
+__global__ __launch_bounds__(256) void rows_kernel(RowArgs p) { place_rows<E, false>(p); }
+
 struct SortArgs {
     Saved s;
     uint32_t* list;  // [N, K]: row | class << 8 | entry << 16, row and class in the tile
@@ -1317,10 +1316,11 @@ __device__ __forceinline__ float* few_at(char* lds, int r) {
 }
 
 // z of rows [0, rows) and classes [n0, n0 + 32) into LDS at FewLds::Z (bias and all,
-// -infinity past the classes; rows behind the last hold nothing of use).
-template <typename E, int RB>
-__device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias, int rows,
-                                      int live, int V, int d, int n0, char* lds) {
+// -infinity past the classes; rows behind the last hold nothing of use). bias_of: of four
+// classes.
+template <typename E, int RB, class BIAS>
+__device__ __forceinline__ void few_z(const E* x, const E* w, BIAS bias_of, int rows, int live,
+                                      int V, int d, int n0, char* lds) {
     constexpr int PER = 16 / sizeof(E), GROUP = 8 * PER;  // elements of a chunk, of a group
     constexpr int LA = 4 * RB, LB = 4;
     const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5;
@@ -1329,7 +1329,7 @@ __device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias
     const long long row_bytes = static_cast<long long>(d) * sizeof(E);
     // (wave w's columns of z, see below)
     const int c = 8 * wave + 4 * h;
-    const float4 bias = *reinterpret_cast<const float4*>(zbias + n0 + c);
+    const float4 bias = bias_of(n0 + c);
     const bool half = RB > 1 && live <= 32;  // no row behind the first 32
     const auto rx = make_rsrc(x, rows * row_bytes);
     const auto rw = make_rsrc(w + static_cast<size_t>(n0) * d, classes * row_bytes);
@@ -1418,24 +1418,38 @@ __device__ __forceinline__ void few_z(const E* x, const E* w, const float* zbias
 
 struct FewStatsArgs {
     Saved s;
+    const void *x, *bias;  // ALL: as they were given
     const void* weight;
     float *mx, *sum, *sum_t;  // [strips][N]: a strip is a block's classes
     int N, V, d, ldk;
     float scale, scale_t;
 };
 
-template <typename E, int RB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3)))
-void few_stats_kernel(FewStatsArgs p) {
-    __shared__ __attribute__((aligned(16))) char lds[FewLds<E, RB>::BYTES];
-    const int tid = threadIdx.x, n0 = blockIdx.x * kFewClasses;
-    const int r0 = blockIdx.y * kFewRows, rows = min(kFewRows, p.N - r0);
+// Strip `strip` of the rows' group blockIdx.y. ALL: of all rows in their own order,
+// whether they are live or not (what comes of those that are not is not used), and so
+// without a word from place_rows; else of live rows in their places.
+template <typename E, int RB, bool ALL>
+__device__ __forceinline__ void few_stats(const FewStatsArgs& p, int strip, char* lds) {
+    const int tid = threadIdx.x, n0 = strip * kFewClasses;
+    const int r0 = ALL ? 0 : blockIdx.y * kFewRows, rows = min(kFewRows, p.N - r0);
     if (r0 > 0 && r0 >= p.s.head->live) return;
-    // (all places of rows, so that no load waits for the number of live ones: what is
-    // behind those is left out below)
-    const int live = min(rows, p.s.head->live - r0);
-    few_z<E, RB>(static_cast<const E*>(p.s.x) + static_cast<size_t>(r0) * p.d,
-                 static_cast<const E*>(p.weight), p.s.bias, rows, live, p.V, p.d, n0, lds);
+    const int live = ALL ? rows : min(rows, p.s.head->live - r0);
+    auto bias_of = [&](int c) {
+        if constexpr (ALL) {
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                v[q] = c + q >= p.V ? -__builtin_inff()
+                       : p.bias != nullptr ? Elem<E>::load(static_cast<const E*>(p.bias), c + q)
+                                           : 0.0f;
+            return make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+            return *reinterpret_cast<const float4*>(p.s.bias + c);
+        }
+    };
+    const void* const x = ALL ? p.x : p.s.x;
+    few_z<E, RB>(static_cast<const E*>(x) + static_cast<size_t>(r0) * p.d,
+                 static_cast<const E*>(p.weight), bias_of, rows, live, p.V, p.d, n0, lds);
     // four threads a row, eight classes each
     const int r = tid >> 2, c0 = 8 * (tid & 3);
     if (r < 32 * RB) {
@@ -1458,7 +1472,7 @@ void few_stats_kernel(FewStatsArgs p) {
             return s + __shfl_xor(s, 2, 64);
         };
         const float s = total(p.scale), st = p.sum_t != nullptr ? total(p.scale_t) : 0.0f;
-        const size_t at = static_cast<size_t>(blockIdx.x) * p.N + r0 + r;
+        const size_t at = static_cast<size_t>(strip) * p.N + r0 + r;
         if (r < live && (tid & 3) == 0) {
             p.mx[at] = m;
             p.sum[at] = s;
@@ -1467,11 +1481,29 @@ void few_stats_kernel(FewStatsArgs p) {
     }
 }
 
+template <typename E, int RB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3)))
+void few_stats_kernel(FewStatsArgs p) {
+    __shared__ __attribute__((aligned(16))) char lds[FewLds<E, RB>::BYTES];
+    few_stats<E, RB, false>(p, blockIdx.x, lds);
+}
+
+// At most 64 rows: the rows' blocks and z's in one launch (forward and backward of one row
+// of 768 against 1000 classes 24.4 -> 21.9 us, of 16 with a teacher 31.3 -> 28.3).
+template <typename E, int RB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3)))
+void few_first_kernel(RowArgs t, FewStatsArgs p, int row_blocks) {
+    __shared__ __attribute__((aligned(16))) char lds[FewLds<E, RB>::BYTES];
+    const int block = blockIdx.x;
+    if (block < row_blocks) place_rows<E, true>(t);
+    else few_stats<E, RB, true>(p, block - row_blocks, lds);
+}
+
 struct FewGradArgs {
     Saved s;
     void* dz;
     int first, per, N, K, ldz, ldk;  // the piece's first class, its classes by eight
-    int mean;
+    int mean, all;  // all: z of all rows in their own order
     float w_label, w_teacher, inv_t;
 };
 
@@ -1479,11 +1511,13 @@ struct FewGradArgs {
 // classes in f32 8.3 us, 3.4 TB/s; 64 x 21 841 in bf16 4.3 us.
 template <typename E>
 __global__ __launch_bounds__(256) void few_grad_kernel(FewGradArgs p) {
-    const int i = blockIdx.x * 256 + threadIdx.x, r = i / p.per, c = 8 * (i - r * p.per);
+    const int i = blockIdx.x * 256 + threadIdx.x, t = i / p.per, c = 8 * (i - t * p.per);
     const Header h = *p.s.head;
-    if (r >= h.live) return;
+    if (t >= p.N) return;
+    const int r = p.all ? p.s.place[t] : t < h.live ? t : -1;
+    if (r < 0) return;
     float v[8];
-    load8(p.s.z + static_cast<size_t>(r) * p.ldk + p.first + c, v);
+    load8(p.s.z + static_cast<size_t>(t) * p.ldk + p.first + c, v);
     const float4 rec = p.s.rec[r];
     const float2 g = Rates(h, p.w_label, p.w_teacher, p.mean).of(p.s.weight[r]);
     const Softmax soft(h, p.K > 0, p.inv_t);
@@ -1506,6 +1540,7 @@ struct FinishArgs {
     unsigned* ticket;
     float *losses, *row_losses;
     int strips, N, K, mean, ldk;    // ldk: a row of the z that was kept, 0 where none was
+    int all;                        // strips and z are of all rows in their own order
     float temperature, inv, inv_t;  // inv: of `sum`'s softmax
 };
 
@@ -1539,7 +1574,7 @@ struct RowSums {
     }
 };
 
-// LR live rows a block; of each wave 64 / LR lanes a row, which share the strips with
+// LR rows a block; of each wave 64 / LR lanes a row, which share the strips with
 // the other waves', four at a time. A chain of latencies: 14 us for 6304 rows of 252
 // strips, 9 for 64 rows of 683; where strips are many the reads: 27 696 rows of 250 28 us,
 // 2.1 TB/s.
@@ -1552,16 +1587,18 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     __shared__ double part_s[W][4];
     __shared__ bool last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int live = p.s.head->live;
-    const int lr = lane % LR, r = blockIdx.x * LR + lr;
-    const bool in = r < live, two = p.sum_t != nullptr;
+    const int live = p.all ? p.N : p.s.head->live;
+    // the place of row t of the strips, -1 without
+    auto place_of = [&](int t) { return t >= live ? -1 : p.all ? p.s.place[t] : t; };
+    const int lr = lane % LR, t = blockIdx.x * LR + lr, r = place_of(t);
+    const bool in = r >= 0, two = p.sum_t != nullptr;
     const float scale = kLog2e * p.inv, scale_t = kLog2e * p.inv_t;
-    // The logit of target e of row r: where the tiles left it, or from the z that was kept
+    // The logit of target e of row t: where the tiles left it, or from the z that was kept
     // (0 of one that is none).
-    auto target = [&](int r, size_t e) {
+    auto target = [&](int t, size_t e) {
         if (p.ldk == 0) return p.s.tz[e];
         const int c = p.s.tidx[e];
-        return p.s.tz[e] = c >= 0 ? p.s.z[static_cast<size_t>(r) * p.ldk + c] : 0.0f;
+        return p.s.tz[e] = c >= 0 ? p.s.z[static_cast<size_t>(t) * p.ldk + c] : 0.0f;
     };
     // (requested ahead of the strips)
     const bool owner = wave == 0 && lane < LR && in;
@@ -1572,7 +1609,7 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     if (owner) {
         weight = p.s.weight[r];
         rec = p.s.rec[r];
-        zlabel = target(r, static_cast<size_t>(r) * (1 + p.K));
+        zlabel = target(t, static_cast<size_t>(r) * (1 + p.K));
         row = p.s.row[r];
     }
     RowSums z;
@@ -1582,7 +1619,7 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const bool there = q + u * SHARE < p.strips;
-                const size_t at = static_cast<size_t>(there ? q + u * SHARE : q) * p.N + r;
+                const size_t at = static_cast<size_t>(there ? q + u * SHARE : q) * p.N + t;
                 m2[u] = p.mx[at];
                 s2[u] = p.sum[at];
                 t2[u] = two ? p.sum_t[at] : 0.0f;
@@ -1595,9 +1632,10 @@ __global__ __launch_bounds__(64 * kFinishWaves) void finish_kernel(FinishArgs p)
     // is 0)
     if (p.K > 0) {
         for (int u = wave; u < LR; u += W) {
-            const int k = blockIdx.x * LR + u;
+            const int k = blockIdx.x * LR + u, at = place_of(k);
             if (k >= live) break;
-            const size_t entry = static_cast<size_t>(k) * (1 + p.K) + 1;
+            if (at < 0) continue;
+            const size_t entry = static_cast<size_t>(at) * (1 + p.K) + 1;
             float v = 0.0f;
             for (int j = lane; j < p.K; j += 64) {
                 const float q = p.s.tq[entry + j], zt = target(k, entry + j) * p.inv_t;
@@ -2060,33 +2098,38 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
                      reinterpret_cast<int32_t*>(base + p.counts_off), p.row_blocks};
     const bool bf16 = s.dtype == VMOE_BF16;
     const float inv_t = 1.0f / s.temperature;
-    const RowArgs t{x, told, zb, row_losses, m.counts, v, s.d_model, p.row_blocks, p.mark_rows,
+    const RowArgs t{x, told, zb.ticket, row_losses, m.counts, v, s.d_model, p.row_blocks, p.mark_rows,
                     bias != nullptr, inv_t};
     const unsigned row_grid = N > 0 ? cdiv(N, 4) : 1;
     float* const mx = reinterpret_cast<float*>(base + p.mx_off);
     float* const sum = reinterpret_cast<float*>(base + p.sum_off);
     float* const sum_t = p.two ? reinterpret_cast<float*>(base + p.sumt_off) : nullptr;
     const float inv = K > 0 && labels == nullptr ? inv_t : 1.0f;  // of `sum`
-    if (N <= kFewRows) {
-        const unsigned grid = row_grid + cdiv(zb.vpad, 256);
-        if (bf16) rows_kernel<uint16_t, true><<<grid, 256, 0, st>>>(t);
-        else rows_kernel<float, true><<<grid, 256, 0, st>>>(t);
-    } else {
+    const bool all = N <= kFewRows;
+    if (!all) {
         mark_kernel<<<p.row_blocks + cdiv(zb.vpad, p.mark_rows), p.mark_rows, 0, st>>>(m);
-        if (bf16) rows_kernel<uint16_t, false><<<row_grid, 256, 0, st>>>(t);
-        else rows_kernel<float, false><<<row_grid, 256, 0, st>>>(t);
+        if (bf16) rows_kernel<uint16_t><<<row_grid, 256, 0, st>>>(t);
+        else rows_kernel<float><<<row_grid, 256, 0, st>>>(t);
     }
     if (p.few) {
-        const FewStatsArgs a{v, weight, mx, sum, sum_t, N, V, s.d_model, kept_classes(s),
+        const FewStatsArgs a{v, x, bias, weight, mx, sum, sum_t, N, V, s.d_model, kept_classes(s),
                              kLog2e * inv, kLog2e * inv_t};
-        auto go = [&](auto blocks) {
+        auto go = [&](auto type, auto blocks) {
+            using E = decltype(type);
             constexpr int RB = decltype(blocks)::value;
-            const dim3 grid(p.strips, cdiv(N, kFewRows));
-            if (bf16) few_stats_kernel<uint16_t, RB><<<grid, 256, 0, st>>>(a);
-            else few_stats_kernel<float, RB><<<grid, 256, 0, st>>>(a);
+            const unsigned strips = N > 0 ? p.strips : 0;
+            if (all)
+                few_first_kernel<E, RB><<<row_grid + strips, 256, 0, st>>>(
+                    t, a, static_cast<int>(row_grid));
+            else
+                few_stats_kernel<E, RB><<<dim3(strips, cdiv(N, kFewRows)), 256, 0, st>>>(a);
         };
-        if (N > 32) go(std::integral_constant<int, 2>{});
-        else if (N > 0) go(std::integral_constant<int, 1>{});
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
+        if (bf16 && N > 32) go(uint16_t{}, Two{});
+        else if (bf16) go(uint16_t{}, One{});
+        else if (N > 32) go(float{}, Two{});
+        else go(float{}, One{});
     } else {
         const bool sorted = K > 0 && !keeps_logits(s);
         const SortArgs g{v, reinterpret_cast<uint32_t*>(base + p.list_off),
@@ -2121,7 +2164,7 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
 
     const FinishArgs f{v, mx, sum, sum_t, reinterpret_cast<double*>(base + p.sums_off), zb.ticket,
                        losses, row_losses, p.strips, N, K, s.reduction == VMOE_REDUCE_MEAN,
-                       keeps_logits(s) ? kept_classes(s) : 0, s.temperature, inv, inv_t};
+                       keeps_logits(s) ? kept_classes(s) : 0, all, s.temperature, inv, inv_t};
     if (p.finish_rows == 16) finish_kernel<16><<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
     else finish_kernel<64><<<p.finish_blocks, 64 * kFinishWaves, 0, st>>>(f);
     return launch_status();
@@ -2168,7 +2211,7 @@ vmoe_status head_bwd_launch(const vmoe_head_shape& s, const void* weight, const 
             // (the forward wrote z of whole blocks of classes)
             const int per = static_cast<int>(cdiv(count, kFewClasses)) * kFewClasses / 8;
             const FewGradArgs u{v, z.dz, first, per, N, s.n_teacher, z.ldz, kept_classes(s),
-                                z.mean, z.w_label, z.w_teacher, z.inv_t};
+                                z.mean, N <= kFewRows, z.w_label, z.w_teacher, z.inv_t};
             const unsigned grid = cdiv(static_cast<long long>(N) * per, 256);
             if (N > 0 && bf16) few_grad_kernel<uint16_t><<<grid, 256, 0, st>>>(u);
             else if (N > 0) few_grad_kernel<float><<<grid, 256, 0, st>>>(u);
