@@ -1297,8 +1297,8 @@ __global__ __launch_bounds__(1024) void sort_kernel(SortArgs p) {
 // classes: its four waves share k in 128-byte groups, two in flight in registers, which
 // pass through LDS of the wave's own (16-byte chunks XOR-swizzled by row) to be read back
 // as fragments; the waves' sums meet in LDS and are added in wave order. z is kept, so the
-// backward reads the weights once. 64 x 1024 against 21841 classes: 15.6 us here, 45 MB
-// of weights at 2.9 TB/s; 1024 x 1024 against 1000 forward and backward 100 -> 61 us.
+// backward reads the weights once. 64 x 1024 against 21841 classes: 17 us here, 45 MB of
+// weights at 2.6 TB/s; 1024 x 1024 against 1000 forward and backward 100 -> 61 us.
 constexpr int kFewLd = kFewClasses + 4;  // floats a row of z in LDS
 
 template <typename E, int RB>
@@ -2098,8 +2098,8 @@ vmoe_status head_fwd_launch(const vmoe_head_shape& s, const void* x, const void*
                      reinterpret_cast<int32_t*>(base + p.counts_off), p.row_blocks};
     const bool bf16 = s.dtype == VMOE_BF16;
     const float inv_t = 1.0f / s.temperature;
-    const RowArgs t{x, told, zb.ticket, row_losses, m.counts, v, s.d_model, p.row_blocks, p.mark_rows,
-                    bias != nullptr, inv_t};
+    const RowArgs t{x, told, zb.ticket, row_losses, m.counts, v, s.d_model, p.row_blocks,
+                    p.mark_rows, bias != nullptr, inv_t};
     const unsigned row_grid = N > 0 ? cdiv(N, 4) : 1;
     float* const mx = reinterpret_cast<float*>(base + p.mx_off);
     float* const sum = reinterpret_cast<float*>(base + p.sum_off);
